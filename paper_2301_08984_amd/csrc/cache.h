@@ -1,0 +1,72 @@
+// Kernel-side view of the paged cache (include/ss_cache.h), the rule that finds a row in it, and the launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ssa {
+
+struct CacheP {
+  void *kc, *vc;    // codes [n_pages][HK][page][D]
+  float *ks, *vs;   // scales [n_pages][HK][page]; NULL: bf16
+  const int32_t* table;
+  int n_pages, page, shift, HK, D, format, n_seq, max_pages;  // page = 1 << shift
+};
+
+// The pool's page that holds position `pos` of sequence b; -1: none.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int cache_page(const int32_t* table, int n_pages, int shift, int max_pages, int b, int64_t pos) {
+  if (pos < 0 || pos >> shift >= max_pages) return -1;
+  const int page = table[(int64_t)b * max_pages + (pos >> shift)];
+  return page >= 0 && page < n_pages ? page : -1;
+}
+// The row (of D codes, and of one scale) of head h and position `pos` in page `page`.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int64_t cache_row(int page, int shift, int HK, int h, int64_t pos) {
+  return (((int64_t)page * HK + h) << shift) + (pos & ((1 << shift) - 1));
+}
+
+struct CacheRowsP {  // write, read
+  CacheP c;
+  void *K, *V;  // bf16, packed tokens
+  int64_t st, sh;
+  const int32_t *cu, *start;
+  int T;
+};
+hipError_t launch_cache_write(const CacheRowsP& p, hipStream_t st);
+hipError_t launch_cache_read(const CacheRowsP& p, hipStream_t st);
+
+struct CacheAttnP {
+  CacheP c;
+  const void* Q;
+  void* Y;
+  float* lse;
+  const int32_t *cu, *lens;
+  const uint64_t* tree;
+  int64_t q_st, q_sh, y_st, y_sh;
+  float scale;
+  int T, H, G, max_new;
+  char* ws;
+};
+size_t cache_attn_bytes(const CacheAttnP& p);
+hipError_t launch_cache_attn(const CacheAttnP& p, hipStream_t st);
+
+#ifdef __HIPCC__
+// The sequence whose packed tokens, by the n_seq + 1 offsets `cu`, hold row t (the same in all lanes of the wavefront);
+// -1: none.  64 offsets at a time: those that are at most t come first.
+__device__ inline int packed_owner(const int32_t* cu, int n_seq, int t) {
+  const int lane = threadIdx.x & 63;
+  int b = -1;
+  for (int b0 = 0; b0 < n_seq; b0 += 64) {
+    const int i = b0 + lane;
+    const uint64_t before = __builtin_amdgcn_ballot_w64(i < n_seq && cu[min(i, n_seq - 1)] <= t && t < cu[min(i, n_seq - 1) + 1]);
+    if (before) return b0 + 63 - __builtin_clzll(before);
+  }
+  return b;
+}
+#endif
+
+}  // namespace ssa

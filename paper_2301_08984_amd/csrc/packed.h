@@ -1,0 +1,43 @@
+// Kernel-side view of one chunk of key heads of attention over packed sequences (include/ss_packed.h), and the
+// launchers.  Filled by packed_api.hip, passed by value to every kernel.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ssa {
+
+struct PackedP {
+  const void *Q, *K, *V, *Y, *dY;
+  void *Yo, *dQ, *dK, *dV;  // Yo: the forward's output
+  const int32_t *cu_q, *cu_k;
+  int64_t q_st, q_sh, k_st, k_sh, y_st, y_sh;  // strides of (Q, dQ), (K, V, dK, dV), (Y, dY)
+  // softmax statistics, query head h and row t at (h - s_h0) * Tq + t; `lse_out` may be NULL
+  float *lse_out, *delta_out;
+  const float *lse, *delta;
+  int lse_h0, delta_h0;
+  float scale;
+  int Tq, Tk, n_seq, H, HK, D, G;  // G = H / HK
+  int h0, h1;                      // the chunk's key heads
+};
+
+hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st);    // Yo, and lse_out if given
+hipError_t launch_packed_stat(const PackedP& p, hipStream_t st);   // lse_out and delta_out, recomputed
+hipError_t launch_packed_delta(const PackedP& p, hipStream_t st);  // delta_out from Y and dY
+hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);
+hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st);
+
+#ifdef __HIPCC__
+// One sequence: its first query row and queries, its first key row and keys.  Offsets are clamped, so that no row
+// outside the tensors is named whatever the array holds.
+struct PackedSeq { int q0, n, k0, m; };
+__device__ inline PackedSeq packed_seq(const PackedP& p, int b) {
+  PackedSeq s;
+  s.q0 = min(max(p.cu_q[b], 0), p.Tq);
+  s.n = max(min(p.cu_q[b + 1], p.Tq) - s.q0, 0);
+  s.k0 = min(max(p.cu_k[b], 0), p.Tk);
+  s.m = max(min(p.cu_k[b + 1], p.Tk) - s.k0, 0);
+  return s;
+}
+#endif
+
+}  // namespace ssa
