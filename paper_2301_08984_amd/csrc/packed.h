@@ -22,8 +22,7 @@ struct PackedP {
 
 hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st);    // Yo, and lse_out if given
 hipError_t launch_packed_stat(const PackedP& p, hipStream_t st);   // lse_out and delta_out, recomputed
-hipError_t launch_packed_delta(const PackedP& p, hipStream_t st);  // delta_out from Y and dY
-hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);
+hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);     // dQ; with Y given delta_out too, else from delta
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st);
 
 #ifdef __HIPCC__

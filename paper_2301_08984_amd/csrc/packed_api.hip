@@ -27,7 +27,11 @@ int validate(const ss_packed_desc* d) {
   const int64_t lim = (int64_t)1 << 24;
   if (d->q_stride_t >= lim || d->q_stride_h >= lim || d->k_stride_t >= lim || d->k_stride_h >= lim || d->y_stride_t >= lim || d->y_stride_h >= lim)
     return SS_ERR_UNSUPPORTED;
-  if (d->Tq > (1 << 30) || d->Tk > (1 << 30)) return SS_ERR_UNSUPPORTED;
+  // ... and a step's 32 rows of (token, head) pairs too; rows and work-groups are counted in 31 bits
+  const int64_t G = d->H / d->HK;
+  if (G * d->q_stride_h + 33 * d->q_stride_t >= (int64_t)1 << 30 || G * d->y_stride_h + 33 * d->y_stride_t >= (int64_t)1 << 30) return SS_ERR_UNSUPPORTED;
+  if (d->Tq > (1 << 30) || d->Tk > (1 << 30) || d->Tq * G >= (1 << 30)) return SS_ERR_UNSUPPORTED;
+  if ((((d->Tq * G > d->Tk ? d->Tq * G : d->Tk) >> 7) + d->n_seq + 8) * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   if (d->lo < 0 || d->lo >= d->hi || d->hi > d->HK) return SS_ERR_BAD_RANGE;
   if (d->k < 1 || d->k > d->hi - d->lo) return SS_ERR_BAD_K;
   return SS_OK;
@@ -136,8 +140,7 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
     p.delta_out = (float*)(ws + w.delta);
     p.delta = p.delta_out;
     if (lse) {
-      p.lse = lse;
-      PK_LAUNCH(ssa::launch_packed_delta(p, st), "delta");
+      p.lse = lse;  // (Delta: by the kernel of dQ)
     } else {
       p.lse_h0 = p.h0 * p.G;
       p.lse_out = (float*)(ws + w.lse);
