@@ -16,8 +16,10 @@
  *
  * One call runs one GPU's share, the key heads [lo,hi) with their query heads, as k sub-operators along that
  * axis (op-trans, op-order; ss_attn.h): the scratch of the backward is that of one chunk and shrinks as 1/k, and the
- * results are the same bits for every k.  All pointers are DEVICE pointers, the descriptor and size outputs
- * HOST memory; no call allocates, synchronises or keeps state.  Error codes are those of ss_attn.h.
+ * results are the same bits for every k.  (Chunks run together where their scratch fits the workspace at hand, or the buffer that
+ * the library holds on each GPU, unless another stream is using it or the call is being captured into a graph.)  All pointers
+ * are DEVICE pointers, the descriptor and size outputs HOST memory; no call allocates or synchronises, and that buffer is the
+ * only state.  Error codes are those of ss_attn.h.
  */
 #ifndef SS_PACKED_H
 #define SS_PACKED_H
@@ -49,8 +51,7 @@ typedef struct {
   uint32_t flags;    /* 0                                                            */
 } ss_packed_desc;
 
-/* Workspace bytes (host outputs, either may be NULL).  Forward: 0.  Backward: one chunk's statistics
- * (LSE and Delta), and the partial sums of dK and dV where few key heads leave the chip idle otherwise. */
+/* Workspace bytes (host outputs, either may be NULL).  Forward: 0.  Backward: one chunk's statistics (LSE and Delta). */
 int ss_packed_workspace_bytes(const ss_packed_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes);
 
 /* The key heads of chunk c (0 <= c < k): lo + floor(c*n/k) .. lo + floor((c+1)*n/k), n = hi-lo. */

@@ -18,6 +18,7 @@ struct PackedP {
   float scale;
   int Tq, Tk, n_seq, H, HK, D, G;  // G = H / HK
   int h0, h1;                      // the chunk's key heads
+  int share_heads;                 // key heads of the whole share: kernel-shape choices go by it, never by the chunk
 };
 
 hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st);    // Yo, and lse_out if given

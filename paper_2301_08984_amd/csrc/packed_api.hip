@@ -6,6 +6,7 @@
 #include <cstdio>
 
 #include "packed.h"
+#include "shared_scratch.h"
 
 namespace {
 
@@ -37,23 +38,26 @@ int validate(const ss_packed_desc* d) {
   return SS_OK;
 }
 
-void chunk(const ss_packed_desc* d, int c, int* a, int* b) {
+void chunk(const ss_packed_desc* d, int k, int c, int* a, int* b) {
   const int64_t n = d->hi - d->lo;
-  *a = d->lo + (int)((c * n) / d->k);
-  *b = d->lo + (int)(((c + 1) * n) / d->k);
+  *a = d->lo + (int)((c * n) / k);
+  *b = d->lo + (int)(((c + 1) * n) / k);
 }
 
+// The scratch of one chunk: LSE (unless the caller kept it) and Delta of its query heads.
 struct Ws {
   size_t lse, delta, total;
 };
-Ws layout(const ss_packed_desc* d) {
-  const int64_t n = d->hi - d->lo, most = (n + d->k - 1) / d->k;  // key heads of the largest chunk
+Ws layout(const ss_packed_desc* d, int k, bool kept) {
+  const int64_t n = d->hi - d->lo, most = (n + k - 1) / k;  // key heads of the largest chunk
   const size_t stat = align256((size_t)(most * (d->H / d->HK)) * d->Tq * 4);
-  Ws w;
-  w.lse = 0;
-  w.delta = stat;
-  w.total = 2 * stat;
-  return w;
+  return Ws{stat, 0, kept ? stat : 2 * stat};
+}
+// The fewest chunks, at most d->k, whose scratch fits `bytes`: 1, 2, 4, .. (every number gives the same results).
+int fewest_chunks(const ss_packed_desc* d, bool kept, size_t bytes) {
+  for (int k = 1; k < d->k; k *= 2)
+    if (layout(d, k, kept).total <= bytes) return k;
+  return d->k;
 }
 
 int hip_fail(hipError_t e, const char* what) {
@@ -77,6 +81,7 @@ PackedP params(const ss_packed_desc* d) {
   p.Tq = d->Tq; p.Tk = d->Tk; p.n_seq = d->n_seq;
   p.H = d->H; p.HK = d->HK; p.D = d->D; p.G = d->H / d->HK;
   p.h0 = d->lo; p.h1 = d->hi;
+  p.share_heads = d->hi - d->lo;
   return p;
 }
 
@@ -88,7 +93,7 @@ int ss_packed_workspace_bytes(const ss_packed_desc* d, size_t* fwd_bytes, size_t
   const int rc = validate(d);
   if (rc != SS_OK) return rc;
   if (fwd_bytes) *fwd_bytes = 0;
-  if (bwd_bytes) *bwd_bytes = layout(d).total;
+  if (bwd_bytes) *bwd_bytes = layout(d, d->k, false).total;
   return SS_OK;
 }
 
@@ -98,7 +103,7 @@ int ss_packed_chunk_range(const ss_packed_desc* d, int32_t c, int32_t* lo, int32
   if (!lo || !hi) return SS_ERR_NULL;
   if (c < 0 || c >= d->k) return SS_ERR_BAD_K;
   int a, b;
-  chunk(d, c, &a, &b);
+  chunk(d, d->k, c, &a, &b);
   *lo = a; *hi = b;
   return SS_OK;
 }
@@ -127,19 +132,34 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
   if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(Y) || misaligned(dY) || misaligned(dQ) || misaligned(dK) || misaligned(dV) ||
       (!cu_k && d->Tk != d->Tq))
     return SS_ERR_BAD_SHAPE;
-  const Ws w = layout(d);
-  if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255)) return SS_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < layout(d, d->k, false).total || ((uintptr_t)workspace & 255)) return SS_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)hip_stream;
+  // A chunk of few heads leaves most of the chip idle, and what keeps chunks apart is only that they reuse one chunk's scratch:
+  // run the fewest whose scratch fits the caller's workspace, or else half of the library's buffer if nobody is using it.
+  // SPEEDUP
+  const bool kept = lse != nullptr;
   char* ws = (char*)workspace;
+  int k = fewest_chunks(d, kept, workspace_bytes);
+  const int ks = k > 1 ? fewest_chunks(d, kept, ssa::SHARED_HALF) : k;
+  ssa::SharedUse shared;
+  if (ks < k) {
+    char* own = shared.take(st, ssa::SHARED_FIRST);
+    if (!own) own = shared.take(st, ssa::SHARED_SECOND);
+    if (own) {
+      ws = own;
+      k = ks;
+    }
+  }
+  const Ws w = layout(d, k, kept);
   PackedP p = params(d);
   p.Q = Q; p.K = K; p.V = V; p.Y = Y; p.dY = dY; p.dQ = dQ; p.dK = dK; p.dV = dV;
   p.cu_q = cu_q; p.cu_k = cu_k ? cu_k : cu_q;
-  for (int c = 0; c < d->k; ++c) {
-    chunk(d, c, &p.h0, &p.h1);
+  for (int c = 0; c < k; ++c) {
+    chunk(d, k, c, &p.h0, &p.h1);
     p.delta_h0 = p.h0 * p.G;
     p.delta_out = (float*)(ws + w.delta);
     p.delta = p.delta_out;
-    if (lse) {
+    if (kept) {
       p.lse = lse;  // (Delta: by the kernel of dQ)
     } else {
       p.lse_h0 = p.h0 * p.G;

@@ -1,11 +1,15 @@
 // dK and dV of attention over packed sequences: a wavefront for each gradient, the probabilities handed over through LDS (the scheme
 // of fast_kv128.hip).
 //
-// A work-group of eight wavefronts owns 128 keys of one key head.  Of the two wavefronts of a 32-key block the first forms S = Q K^T and P, hands P
-// over in fp32 and adds dY^T P to dV; the second forms dP = dY V^T, takes P a step later, forms dS and adds Q^T dS to dK.
-// The rows that see the keys go by in steps of 32 (token, head) pairs, all G heads of a token one after the other, so that the sums over the heads
-// are the accumulators' own, without atomics and in a fixed order.  Q and dY rows travel straight into a ring of four LDS slots, two
-// steps ahead, one barrier a step; the second wavefronts are a step behind the first ones.
+// A work-group has eight wavefronts, four pairs.  The first of a pair forms S = Q K^T and P for 32 keys and 32 rows, hands P over in fp32 and
+// adds dY^T P to dV; the second forms dP = dY V^T, takes P a step later, forms dS and adds Q^T dS to dK.  The rows that
+// see the keys go by in steps of 32 (token, head) pairs, all G heads of a token one after the other, so that the sums over the heads
+// are the accumulators' own, without atomics and in a fixed order.  Q and dY rows travel straight into a ring of LDS slots, one
+// or two steps ahead, one barrier a step; the second wavefronts are a step behind the first ones.
+//
+// KB x RG: the pairs take KB blocks of 32 keys, and RG groups of them every RG-th step each; the groups' sums are added up
+// through LDS at the end, in order.  With few keys and key heads a work-group of 128 keys walks far more rows than there are
+// work-groups to fill the chip; the rows are then read by more work-groups.
 #include "packed_tile.h"
 
 #include <type_traits>
@@ -13,15 +17,17 @@
 namespace ssa {
 namespace {
 
-template <int D>
+template <int D, int RG>
 struct KvLds {
-  static constexpr int SLOTS = 4, SLOT_B = 2 * PTile<D>::SUB_B;  // Q and dY rows of a step
-  static constexpr int P_AT = SLOTS * SLOT_B;                    // two slots of P: 32 x 32 fp32 for each of the four key blocks
-  static constexpr int STAT = P_AT + 2 * 4 * 4096;               // of a step: -LSE (base 2) [32], Delta [32], last key seen [32]
-  static constexpr int BYTES = STAT + SLOTS * 384;
+  static constexpr int SLOTS = D * RG == 256 ? 3 : 4, AHEAD = SLOTS - 2;  // three where four do not fit
+  static constexpr int PERIOD = SLOTS == 3 ? 6 : 4;                       // steps after which slots and P's two slots come round
+  static constexpr int SLOT_B = 2 * PTile<D>::SUB_B, RING_B = SLOTS * SLOT_B;  // Q and dY rows of a step; of a group
+  static constexpr int P_AT = RG * RING_B;         // two slots of P: 32 x 32 fp32 for each of the four pairs
+  static constexpr int STAT = P_AT + 2 * 4 * 4096;  // of a group and step: -LSE (base 2) [32], Delta [32], last key seen [32]
+  static constexpr int BYTES = STAT + RG * SLOTS * 384;
 };
 
-// rows of (token, head) pairs, 32 further on with every step
+// rows of (token, head) pairs, a fixed number further on with every step
 struct RowWalk {
   int tok, g;
   __device__ __forceinline__ void init(int row, int G) {
@@ -46,35 +52,43 @@ __device__ __forceinline__ void quads_issue(u32x4 (&f)[4], uint32_t at) {
                : "memory");
 }
 
-template <int D, bool DK>  // DK: the second wavefront of a key block
+template <int D, int RG, bool DK>  // DK: the second wavefront of a pair
 __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, const PackedSeq& s, int tile, int hk) {
   using T = PTile<D>;
-  using L = KvLds<D>;
-  constexpr int KS = T::KS, DB = T::DB, NF = D == 128 ? 2 : 1;  // load instructions of a wavefront and step
+  using L = KvLds<D, RG>;
+  constexpr int KS = T::KS, DB = T::DB, KB = 4 / RG, TK = 32 * KB;
+  constexpr int MATES = 8 / RG, NF = 2 * T::LOADS / MATES;  // wavefronts of a group; load instructions of one in a step
+  constexpr int NR = NF > 1 ? NF / 2 : 1;                   // ... of Q and of dY (D = 64, one group: of one of them)
   const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kblock = w & 3;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kblock = (w & 3) % KB, group = (w & 3) / KB, mate = (DK ? KB : 0) + kblock;
   const int G = p.G, rows = s.n * G, more = s.m - s.n;
-  const int k0 = tile * 128 + 32 * kblock, key = k0 + r;
+  const int k0 = tile * TK + 32 * kblock, key = k0 + r;
   const float c1 = p_factor(p.scale);
-  const int tok0 = max(tile * 128 - more, 0);  // the first token that sees the tile's first key
-  const int first = tok0 < s.n ? tok0 * G / 32 : 0, n = tok0 < s.n ? (rows + 31) / 32 - first : 0;  // steps
-  const int dtok = 32 / G, dg = 32 % G;
+  const int tok0 = max(tile * TK - more, 0);  // the first token that sees the tile's first key
+  const int first = tok0 < s.n ? tok0 * G / 32 : 0, steps = tok0 < s.n ? (rows + 31) / 32 - first : 0;
+  const int n = (steps + RG - 1) / RG, row0 = 32 * (first + group);  // of a group; a group's step t begins at row row0 + 32 RG t
+  const int dtok = 32 * RG / G, dg = 32 * RG % G;
+  char* ring = smem + group * L::RING_B;
 
-  // this wavefront's share of a step: D = 128: rows 4w .. 4w + 3 of Q and of dY; D = 64: rows 8 kblock .. + 7 of Q (first kind) or dY
   const uint32_t qs2 = (uint32_t)p.q_st * 2u, qh2 = (uint32_t)p.q_sh * 2u, ys2 = (uint32_t)p.y_st * 2u, yh2 = (uint32_t)p.y_sh * 2u;
-  const int rho = T::ROWS * (D == 128 ? w : kblock) + lane / T::CHUNKS, chunk = (lane % T::CHUNKS) ^ p_sw<D>(rho);
-  const bool column = 8 * chunk < p.D;
   const int64_t qbase = (int64_t)s.q0 * p.q_st + (int64_t)hk * G * p.q_sh, ybase = (int64_t)s.q0 * p.y_st + (int64_t)hk * G * p.y_sh;
-  RowWalk base, mine, own;  // the step's first row (uniform), the row this lane fetches, the row whose statistics it fetches
-  base.init(32 * first, G);
-  mine.init(32 * first + rho, G);
-  own.init(32 * first + r, G);
+  // this wavefront's load instructions: the group's instructions mate, mate + MATES, .., Q's before dY's
+  RowWalk base, mine[NR], own;  // the step's first row (uniform), the rows this lane fetches, the row whose statistics it fetches
+  uint32_t c16[NR];
+  base.init(row0, G);
+  own.init(row0 + r, G);
+#pragma unroll
+  for (int u = 0; u < NR; ++u) {
+    const int rho = T::ROWS * ((mate + MATES * u) % T::LOADS) + lane / T::CHUNKS, chunk = (lane % T::CHUNKS) ^ p_sw<D>(rho);
+    mine[u].init(row0 + rho, G);
+    c16[u] = 8 * chunk < p.D ? 16u * (uint32_t)chunk : P_NOWHERE;
+  }
   float pstat = 0.f;
   int pseen = 0;
-  // step t into its slot, in order (past the last step and the last row: zeros arrive); the statistics travel through registers of one
-  // wavefront of each kind, asked for before the rows so that waiting for them leaves those under way
+  // the group's step t into its slot, in order (past the last step and the last row: zeros arrive); the statistics travel through registers of
+  // one wavefront of each kind, asked for before the rows so that waiting for them leaves those under way
   auto fetch = [&](char* slot, int t) {
-    const int left = rows - 32 * (first + t);
+    const int left = rows - (row0 + 32 * RG * t);
     if (kblock == 0) {
       const bool there = r < left;
       const int64_t at = (int64_t)(hk * G + own.g - (DK ? p.delta_h0 : p.lse_h0)) * p.Tq + s.q0 + own.tok;
@@ -82,27 +96,35 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
       pseen = there ? own.tok + more : -1;
       own.step(G, dtok, dg);
     }
-    const uint32_t dt = (uint32_t)(mine.tok - base.tok);
-    const bool there = column && rho < left;
-    if (D == 128 || !DK) {
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)p.Q + qbase + (int64_t)base.tok * p.q_st), 0, 0x7e000000, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (w_lds_void*)(slot + (D == 128 ? w : kblock) * 1024), 16,
-                                               there ? dt * qs2 + (uint32_t)mine.g * qh2 + 16u * (uint32_t)chunk : P_NOWHERE, 0, 0, 0);
-    }
-    if (D == 128 || DK) {
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)p.dY + ybase + (int64_t)base.tok * p.y_st), 0, 0x7e000000, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (w_lds_void*)(slot + T::SUB_B + (D == 128 ? w : kblock) * 1024), 16,
-                                               there ? dt * ys2 + (uint32_t)mine.g * yh2 + 16u * (uint32_t)chunk : P_NOWHERE, 0, 0, 0);
+    const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)p.Q + qbase + (int64_t)base.tok * p.q_st), 0, 0x7e000000, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)p.dY + ybase + (int64_t)base.tok * p.y_st), 0, 0x7e000000, 0x00020000);
+    uint32_t oq[NR], oy[NR];
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      const int rho = T::ROWS * ((mate + MATES * u) % T::LOADS) + lane / T::CHUNKS;
+      const uint32_t dt = (uint32_t)(mine[u].tok - base.tok), g = (uint32_t)mine[u].g;
+      const bool there = rho < left && c16[u] != P_NOWHERE;
+      oq[u] = there ? dt * qs2 + g * qh2 + c16[u] : P_NOWHERE;
+      oy[u] = there ? dt * ys2 + g * yh2 + c16[u] : P_NOWHERE;
+      mine[u].step(G, dtok, dg);
     }
     base.step(G, dtok, dg);
-    mine.step(G, dtok, dg);
+#pragma unroll
+    for (int u = 0; u < NR; ++u)
+      if (NF > 1 || !DK)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (w_lds_void*)(slot + ((mate + MATES * u) % T::LOADS) * 1024), 16, oq[u], 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < NR; ++u)
+      if (NF > 1 || DK)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (w_lds_void*)(slot + T::SUB_B + ((mate + MATES * u) % T::LOADS) * 1024), 16, oy[u], 0, 0, 0);
   };
   const uint32_t lds0 = (uint32_t)(size_t)(w_lds_void*)smem;
   uint32_t ka[KS], va[2][DB];
-  p_nat_addr<D>(ka, smem, r, hl);
-  p_tr_addr<D>(va, smem, lane);
-  const uint32_t pa_ = lds0 + L::P_AT + 4096u * kblock + 16u * lane;
-  const uint32_t st_w = lds0 + L::STAT + (DK ? 128u : 0u) + 4u * r, st_r = lds0 + L::STAT + (DK ? 128u : 0u) + 16u * hl;
+  p_nat_addr<D>(ka, ring, r, hl);
+  p_tr_addr<D>(va, ring, lane);
+  const uint32_t pa_ = lds0 + L::P_AT + 4096u * (w & 3) + 16u * lane;
+  const uint32_t stat0 = lds0 + L::STAT + (uint32_t)group * (L::SLOTS * 384) + (DK ? 128u : 0u);
+  const uint32_t st_w = stat0 + 4u * r, st_r = stat0 + 16u * hl;
   auto put_stat = [&](auto slot) {
     constexpr int TO = 384 * decltype(slot)::value;
     const float x = DK || pstat == -INFINITY ? pstat : -pstat * LOG2E;  // a row without a key, or behind the last: its probabilities are 0
@@ -130,11 +152,11 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
 
   RowWalk a, e;  // the first and the last row of the step at work (uniform)
-  a.init(32 * first, G);
-  e.init(32 * first + 31, G);
-  // step t: S and dV, or dP and dK of the step before
-  auto work = [&](auto slot) {
-    constexpr int SL = decltype(slot)::value, SO = SL * L::SLOT_B, PO = 16384 * (SL & 1), TO = 384 * SL;
+  a.init(row0, G);
+  e.init(row0 + 31, G);
+  // a step in slot SL, P in slot PS: S and dV, or dP and dK
+  auto work = [&](auto slot, auto pslot) {
+    constexpr int SL = decltype(slot)::value, SO = SL * L::SLOT_B, PO = 16384 * decltype(pslot)::value, TO = 384 * SL;
     const int begin = a.tok + more, end = e.tok + more;
     const uint32_t pp = pa_;
     a.step(G, dtok, dg);
@@ -148,7 +170,7 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
       u32x4 fr[KS];
       p_nat_issue<SO + (DK ? T::SUB_B : 0)>(fr, ka);
       quads_issue<TO, 32>(l4, st_r);
-      if (DK) quads_issue<PO, 1024>(pr, pa_);
+      if (DK) quads_issue<PO, 1024>(pr, pp);
       p_nat_wait(fr);
       asm volatile("" : "+v"(l4[0]), "+v"(l4[1]), "+v"(l4[2]), "+v"(l4[3]));
       if (DK) asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(pr[2]), "+v"(pr[3]));
@@ -188,35 +210,71 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] = mfma(w_frag2(tf[hb][2 * db], tf[hb][2 * db + 1]), of[hb], acc[db]);
   };
-  // step t of the work-group: rows t have landed for everybody, P of step t - 1 is there, and slot t + 2 and P's slot t are free
-  auto step = [&](auto slot, int t) {
-    constexpr int SL = decltype(slot)::value;
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NF) : "memory");
+  // Step t: its rows have landed for everybody and P of step t - 1 is there; the slots of step t + AHEAD and of P t are free.
+  // The statistics of step t are in LDS: written a step before, or, if they were asked for one step ahead only, before the barrier.
+  auto step = [&](auto number, int t) {
+    constexpr int I = decltype(number)::value, SL = I % L::SLOTS;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NF * (L::AHEAD - 1)) : "memory");
+    if (L::AHEAD == 1) put_stat(std::integral_constant<int, SL>{});
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    put_stat(std::integral_constant<int, (SL + 1) & 3>{});
-    fetch(smem + ((SL + 2) & 3) * L::SLOT_B, t + 2);
+    if (L::AHEAD == 2) put_stat(std::integral_constant<int, (SL + 1) % L::SLOTS>{});
+    fetch(ring + ((SL + L::AHEAD) % L::SLOTS) * L::SLOT_B, t + L::AHEAD);
     if (DK) {
-      if (t > 0) work(std::integral_constant<int, (SL + 3) & 3>{});
+      if (t > 0) work(std::integral_constant<int, (SL + L::SLOTS - 1) % L::SLOTS>{}, std::integral_constant<int, (I + 1) & 1>{});
     } else {
-      if (t < n) work(slot);
+      if (t < n) work(std::integral_constant<int, SL>{}, std::integral_constant<int, I & 1>{});
     }
   };
   if (n > 0) {
-    fetch(smem, 0);
-    put_stat(std::integral_constant<int, 0>{});
-    fetch(smem + L::SLOT_B, 1);
+    fetch(ring, 0);
+    if (L::AHEAD == 2) {
+      put_stat(std::integral_constant<int, 0>{});
+      fetch(ring + L::SLOT_B, 1);
+    }
     // (used here, so that the loop holds no wait for them)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kr[ks]));
-    for (int t = 0; t <= n; t += 4) {
+    for (int t = 0; t <= n; t += L::PERIOD) {
       step(std::integral_constant<int, 0>{}, t);
       if (t + 1 <= n) step(std::integral_constant<int, 1>{}, t + 1);
       if (t + 2 <= n) step(std::integral_constant<int, 2>{}, t + 2);
       if (t + 3 <= n) step(std::integral_constant<int, 3>{}, t + 3);
+      if (L::PERIOD == 6) {
+        if (t + 4 <= n) step(std::integral_constant<int, 4>{}, t + 4);
+        if (t + 5 <= n) step(std::integral_constant<int, 5>{}, t + 5);
+      }
     }
-    W_VMCNT(0);  // nothing may still be on its way into LDS when the work-group ends
+    W_VMCNT(0);  // nothing may still be on its way into LDS
+    if (RG > 1) {
+      // the other groups' sums, in the rings' place: a quarter of a block is 64 lanes x 16 bytes
+      float4* part = (float4*)smem + ((((DK ? 1 : 0) * KB + kblock) * RG + group) * DB * 4) * 64 + lane;
+      __syncthreads();
+      if (group > 0) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) part[(4 * db + g) * 64] = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
+      }
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int o = 1; o < RG; ++o)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const float4 x = part[((o * DB + db) * 4 + g) * 64];
+              acc[db][4 * g] += x.x;
+              acc[db][4 * g + 1] += x.y;
+              acc[db][4 * g + 2] += x.z;
+              acc[db][4 * g + 3] += x.w;
+            }
+      }
+    }
   }
+  if (group > 0) return;
   uint16_t* out = (uint16_t*)(DK ? p.dK : p.dV) + (int64_t)(s.k0 + min(key, s.m - 1)) * p.k_st + (int64_t)hk * p.k_sh;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -228,23 +286,30 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
   }
 }
 
-template <int D>
+template <int D, int RG>
 __global__ __launch_bounds__(512, 2) void packed_dkdv_kernel(PackedP p) {
-  __shared__ __attribute__((aligned(1024))) char smem[KvLds<D>::BYTES];
+  __shared__ __attribute__((aligned(1024))) char smem[KvLds<D, RG>::BYTES];
+  static_assert(sizeof(smem) <= 160 * 1024 && (RG == 1 || 8 * 32 * D * 4 <= KvLds<D, RG>::STAT), "the groups' sums fit, too");
   const PPlace at = p_place(p.h1 - p.h0);
-  const PFound f = p_find<true>(p, at.rank);
+  const PFound f = p_find<true, RG == 1 ? 7 : RG == 2 ? 6 : 5>(p, at.rank);
   if (f.t < 0) return;
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8)) packed_kv_wave<D, true>(p, smem, f.s, f.t, p.h0 + at.head);
-  else packed_kv_wave<D, false>(p, smem, f.s, f.t, p.h0 + at.head);
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8)) packed_kv_wave<D, RG, true>(p, smem, f.s, f.t, p.h0 + at.head);
+  else packed_kv_wave<D, RG, false>(p, smem, f.s, f.t, p.h0 + at.head);
+}
+
+template <int D, int RG>
+hipError_t launch(const PackedP& p, hipStream_t st) {
+  packed_dkdv_kernel<D, RG><<<(int)p_blocks(p_most_tiles(p, true, RG == 1 ? 7 : RG == 2 ? 6 : 5), p.h1 - p.h0), 512, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st) {
-  const int g = (int)p_blocks(p_most_tiles(p, true), p.h1 - p.h0);
-  if (p.D <= 64) packed_dkdv_kernel<64><<<g, 512, 0, st>>>(p);
-  else packed_dkdv_kernel<128><<<g, 512, 0, st>>>(p);
-  return hipGetLastError();
+  const int64_t tiles = (int64_t)(p.Tk >> 7) * p.share_heads;
+  if (p.D > 64) return tiles < 512 ? launch<128, 2>(p, st) : launch<128, 1>(p, st);
+  if (tiles < 256) return launch<64, 4>(p, st);
+  return tiles < 512 ? launch<64, 2>(p, st) : launch<64, 1>(p, st);
 }
 
 }  // namespace ssa

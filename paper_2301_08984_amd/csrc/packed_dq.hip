@@ -18,7 +18,7 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const PPlace at = p_place(p.h1 - p.h0);
-  const PFound f = p_find<false>(p, at.rank);
+  const PFound f = p_find<false, 7>(p, at.rank);
   if (f.t < 0) return;
   const PackedSeq s = f.s;
   const int hk = p.h0 + at.head, rows = s.n * p.G, more = s.m - s.n;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void packed_dq_kernel(Packed
 
 template <bool KEPT>
 hipError_t launch(const PackedP& p, hipStream_t st) {
-  const int g = (int)p_blocks(p_most_tiles(p, false), p.h1 - p.h0);
+  const int g = (int)p_blocks(p_most_tiles(p, false, 7), p.h1 - p.h0);
   if (p.D <= 64) packed_dq_kernel<64, KEPT><<<g, 256, 0, st>>>(p);
   else packed_dq_kernel<128, KEPT><<<g, 256, 0, st>>>(p);
   return hipGetLastError();

@@ -144,30 +144,30 @@ __device__ __forceinline__ PPlace p_place(int HK) {
 }
 inline int64_t p_blocks(int64_t tiles, int HK) { return (tiles + 7) / 8 * 8 * HK; }
 
-// The tile of rank `rank`: its sequence, and its number in it (-1: fewer tiles than that).  KEYS: tiles of 128 keys, else of 128
+// The tile of rank `rank`: its sequence, and its number in it (-1: fewer tiles than that).  KEYS: tiles of 1 << SH keys, else of 1 << SH
 // rows.  What a tile costs is the number of its steps: blocks of 64 keys that a tile of rows walks, or of 32 rows that a tile of
 // keys walks.  Up to 64 sequences (a lane each) the tiles are ranked by it, the longest first, so that the chip does not wait for a long one
 // that started last: the number of tiles with at least L steps has a closed form for a sequence, and L is found by
 // bisection.  With more sequences tiles are in the order of the sequences.
 struct PFound { PackedSeq s; int t; };
-template <bool KEYS>
-__device__ __forceinline__ int p_tiles(const PackedSeq& s, int G) { return ((KEYS ? s.m : s.n * G) + 127) >> 7; }
-template <bool KEYS>
+template <bool KEYS, int SH>
+__device__ __forceinline__ int p_tiles(const PackedSeq& s, int G) { return ((KEYS ? s.m : s.n * G) + (1 << SH) - 1) >> SH; }
+template <bool KEYS, int SH>
 __device__ __forceinline__ int p_steps(const PackedSeq& s, int G) {  // of the sequence's heaviest tile
   return KEYS ? (s.n * G + 31) >> 5 : (s.m + 63) >> 6;
 }
-template <bool KEYS>
+template <bool KEYS, int SH>
 __device__ __forceinline__ int p_at_least(const PackedSeq& s, int G, int L) {  // tiles with L steps or more
-  const int tiles = p_tiles<KEYS>(s, G), more = s.m - s.n;
+  const int tiles = p_tiles<KEYS, SH>(s, G), more = s.m - s.n;
   if (L <= 0) return tiles;
   if (KEYS) {
     const int z = s.n - 1 - (32 * (L - 1)) / G;  // the last first token that leaves as many rows
-    return z < 0 || z + more < 0 ? 0 : min(tiles, ((z + more) >> 7) + 1);
+    return z < 0 || z + more < 0 ? 0 : min(tiles, ((z + more) >> SH) + 1);
   }
   const int y = 64 * (L - 1) - more;  // the first token that sees as many keys
-  return y >= s.n ? 0 : tiles - ((max(y, 0) * G) >> 7);
+  return y >= s.n ? 0 : tiles - ((max(y, 0) * G) >> SH);
 }
-template <bool KEYS>
+template <bool KEYS, int SH>
 __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
   const int lane = threadIdx.x & 63, G = p.G;
   PFound f;
@@ -185,27 +185,27 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
   };
   if (p.n_seq <= 64) {
     const PackedSeq s = of_lane(0);
-    if (rank >= p_total(p_tiles<KEYS>(s, G))) return f;
-    int lo = 0, hi = p_steps<KEYS>(s, G);
+    if (rank >= p_total(p_tiles<KEYS, SH>(s, G))) return f;
+    int lo = 0, hi = p_steps<KEYS, SH>(s, G);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) hi = max(hi, __shfl_xor(hi, o));
     hi = __builtin_amdgcn_readfirstlane(hi) + 1;
     while (hi - lo > 1) {  // more than `rank` tiles have `lo` steps or more, not as many have `hi`
       const int mid = (lo + hi) >> 1;
-      if (p_total(p_at_least<KEYS>(s, G, mid)) > rank) lo = mid;
+      if (p_total(p_at_least<KEYS, SH>(s, G, mid)) > rank) lo = mid;
       else hi = mid;
     }
-    const int above = p_at_least<KEYS>(s, G, hi), mine = p_at_least<KEYS>(s, G, lo) - above;
+    const int above = p_at_least<KEYS, SH>(s, G, hi), mine = p_at_least<KEYS, SH>(s, G, lo) - above;
     const int left = rank - p_total(above), upto = p_scan(mine);
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > left));
     from(s, l);
     const int i = left - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)), ab = __builtin_amdgcn_readlane(above, l);
-    f.t = KEYS ? ab + i : p_tiles<KEYS>(f.s, G) - 1 - ab - i;
+    f.t = KEYS ? ab + i : p_tiles<KEYS, SH>(f.s, G) - 1 - ab - i;
     return f;
   }
   for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
     const PackedSeq s = of_lane(b0);
-    const int mine = p_tiles<KEYS>(s, G), upto = p_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+    const int mine = p_tiles<KEYS, SH>(s, G), upto = p_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
     if (rank >= all) {
       rank -= all;
       continue;
@@ -213,13 +213,13 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > rank));
     from(s, l);
     const int i = rank - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
-    f.t = KEYS ? i : p_tiles<KEYS>(f.s, G) - 1 - i;
+    f.t = KEYS ? i : p_tiles<KEYS, SH>(f.s, G) - 1 - i;
     return f;
   }
   return f;
 }
 // (row tiles: 128 * tiles <= Tq * G + 127 * n_seq; key tiles alike)
-inline int64_t p_most_tiles(const PackedP& p, bool keys) { return (keys ? (int64_t)p.Tk : (int64_t)p.Tq * p.G) / 128 + p.n_seq; }
+inline int64_t p_most_tiles(const PackedP& p, bool keys, int sh) { return ((keys ? (int64_t)p.Tk : (int64_t)p.Tq * p.G) >> sh) + p.n_seq; }
 
 // 1 / ln 2 times the scale, never zero: a factor of 0 would make NaN of a masked score; any score times 2^-120 is 0
 // next to the exponents that matter.  Its sign goes into Q.
