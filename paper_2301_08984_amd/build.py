@@ -23,7 +23,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 # that all of a wavefront's registers are vector registers (see the header of fast_wave_fwd128.hip).
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 EXTRA_FLAGS = {"win_fwd.hip": VGPR_FORM, "win_bwd.hip": VGPR_FORM, "pair_dbias.hip": VGPR_FORM, "fast_fwd128.hip": VGPR_FORM, "fast_stat128.hip": VGPR_FORM, "fast_dq128.hip": VGPR_FORM, "fast_kv128.hip": VGPR_FORM, "fast_wave_fwd128.hip": VGPR_FORM, "fast_wave_bwd128.hip": VGPR_FORM,
-               "packed_fwd.hip": VGPR_FORM, "packed_dq.hip": VGPR_FORM, "packed_dkdv.hip": VGPR_FORM}
+               "packed_fwd.hip": VGPR_FORM, "packed_dq.hip": VGPR_FORM, "packed_dkdv.hip": VGPR_FORM, "cache_attn.hip": VGPR_FORM}
 
 
 def _compile(src: str, objdir: str) -> str:

@@ -50,6 +50,10 @@ struct CacheAttnP {
   float scale;
   int T, H, G, max_new;
   char* ws;
+  // how the work is cut (cache_attn.hip): rows of a sequence and key head at most, groups of them, parts to aim at, slots for parts, the
+  // shortest part, and where in the workspace, in floats, the parts' maxima and sums begin
+  int max_rows, groups, parts, slots, least;
+  int64_t ml_at;
 };
 size_t cache_attn_bytes(const CacheAttnP& p);
 hipError_t launch_cache_attn(const CacheAttnP& p, hipStream_t st);

@@ -34,7 +34,9 @@ int validate(const ss_cache_desc* d, const ss_cache_attn_desc* a) {
   if (!a) return SS_ERR_NULL;
   if (a->T < 1 || a->H < 1 || a->H % d->HK || a->max_new < 1 || !std::isfinite(a->scale)) return SS_ERR_BAD_SHAPE;
   if (bad_stride(a->q_stride_t, a->q_stride_h, d->D) || bad_stride(a->y_stride_t, a->y_stride_h, d->D)) return SS_ERR_BAD_SHAPE;
-  if (a->max_new > 64 || a->H > 65535 || a->T > 1 << 30) return SS_ERR_UNSUPPORTED;
+  if (a->max_new > 64 || a->H > 65535 || (int64_t)a->T * a->H >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
+  // (work-groups are counted in 31 bits)
+  if ((int64_t)(520 + d->n_seq) * d->HK * ((a->max_new * (a->H / d->HK) + 63) / 64) >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
 
