@@ -35,6 +35,7 @@ struct CacheRowsP {  // write, read
   int64_t st, sh;
   const int32_t *cu, *start;
   int T;
+  int groups;  // wavefronts of a token (cache_rows.hip)
 };
 hipError_t launch_cache_write(const CacheRowsP& p, hipStream_t st);
 hipError_t launch_cache_read(const CacheRowsP& p, hipStream_t st);
@@ -50,13 +51,14 @@ struct CacheAttnP {
   float scale;
   int T, H, G, max_new;
   char* ws;
-  // how the work is cut (cache_attn.hip): rows of a sequence and key head at most, groups of them, parts to aim at, slots for parts, the
-  // shortest part, and where in the workspace, in floats, the parts' maxima and sums begin
+  // how the work is cut (cache_attn.hip): rows of a sequence and key head at most, groups of 128 of them, parts to aim at, slots for
+  // parts, the shortest part, and where in the workspace, in floats, the parts' maxima and sums begin
   int max_rows, groups, parts, slots, least;
   int64_t ml_at;
 };
 size_t cache_attn_bytes(const CacheAttnP& p);
 hipError_t launch_cache_attn(const CacheAttnP& p, hipStream_t st);
+hipError_t launch_cache_attn_rows(const CacheAttnP& p, int blocks, hipStream_t st);  // more than 32 rows
 
 #ifdef __HIPCC__
 // The sequence whose packed tokens, by the n_seq + 1 offsets `cu`, hold row t (the same in all lanes of the wavefront);

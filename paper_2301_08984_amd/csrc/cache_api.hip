@@ -36,7 +36,7 @@ int validate(const ss_cache_desc* d, const ss_cache_attn_desc* a) {
   if (bad_stride(a->q_stride_t, a->q_stride_h, d->D) || bad_stride(a->y_stride_t, a->y_stride_h, d->D)) return SS_ERR_BAD_SHAPE;
   if (a->max_new > 64 || a->H > 65535 || (int64_t)a->T * a->H >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   // (work-groups are counted in 31 bits)
-  if ((int64_t)(520 + d->n_seq) * d->HK * ((a->max_new * (a->H / d->HK) + 63) / 64) >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
+  if ((int64_t)(1032 + d->n_seq) * d->HK * ((a->max_new * (a->H / d->HK) + 127) / 128) >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
 
@@ -76,7 +76,7 @@ int check_rows(const ss_cache_desc* d, int T, const void* K, const void* V, int6
   const int rc = validate(d);
   if (rc != SS_OK) return rc;
   if (T < 1 || bad_stride(st, sh, d->D)) return SS_ERR_BAD_SHAPE;
-  if (T > 1 << 30) return SS_ERR_UNSUPPORTED;
+  if ((int64_t)T * (d->HK / 2 + 1) >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;  // (wavefronts are counted in 31 bits)
   if (!K || !V || !cu || !table) return SS_ERR_NULL;
   return misaligned(K) || misaligned(V) ? SS_ERR_BAD_SHAPE : SS_OK;
 }
@@ -100,7 +100,7 @@ int ss_cache_write(const ss_cache_desc* d, int32_t T, const void* K, const void*
   int rc = check_rows(d, T, K, V, stride_t, stride_h, cu, table);
   if (rc == SS_OK) rc = check_store(d, k_codes, k_scales, v_codes, v_scales);
   if (rc != SS_OK) return rc;
-  const CacheRowsP p{store(d, table, k_codes, k_scales, v_codes, v_scales), const_cast<void*>(K), const_cast<void*>(V), stride_t, stride_h, cu, start, T};
+  const CacheRowsP p{store(d, table, k_codes, k_scales, v_codes, v_scales), const_cast<void*>(K), const_cast<void*>(V), stride_t, stride_h, cu, start, T, 0};
   return done(ssa::launch_cache_write(p, (hipStream_t)hip_stream), "write");
 }
 
@@ -110,7 +110,7 @@ int ss_cache_read(const ss_cache_desc* d, int32_t T, const int32_t* cu, const in
   int rc = check_rows(d, T, K, V, stride_t, stride_h, cu, table);
   if (rc == SS_OK) rc = check_store(d, k_codes, k_scales, v_codes, v_scales);
   if (rc != SS_OK) return rc;
-  const CacheRowsP p{store(d, table, k_codes, k_scales, v_codes, v_scales), K, V, stride_t, stride_h, cu, start, T};
+  const CacheRowsP p{store(d, table, k_codes, k_scales, v_codes, v_scales), K, V, stride_t, stride_h, cu, start, T, 0};
   return done(ssa::launch_cache_read(p, (hipStream_t)hip_stream), "read");
 }
 

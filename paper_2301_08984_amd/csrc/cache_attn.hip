@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged cache (include/ss_cache.h).
 //
 // Bound by reading the cache: 4 D bytes (2 D + 8 in 8 bits) a key and head for 4 D flops a row, so a key is read once for all rows that see
-// it, the new tokens of a sequence times the G query heads of a key head, 32 or 64 (NQ = 2) to a wavefront, and goes from memory into
+// it, the new tokens of a sequence times the G query heads of a key head, here up to 32 (more: cache_attn_rows.hip), and goes from memory into
 // registers: nothing passes through LDS until the end.  The keys of all sequences are cut into parts of about equal length, so that a long
 // sequence does not keep the chip waiting; the four wavefronts of a work-group take every fourth block of 32 keys of a part each, with a
 // running maximum and sum, and are joined through LDS.  A sequence in one part is finished there; the others' parts are joined by
@@ -11,96 +11,14 @@
 // exactly, and the key's scale multiplies the fp32 score.  O^T += V^T P^T: a lane holds D / 32 neighbouring columns of eight keys, which byte permutes turn
 // into operands (eight keys of a column), so that V needs no transposed copy in LDS; the value's scale goes into P, which is
 // rounded to bf16 as the matrix instructions take it.  Maxima, sums and O are fp32.
-#include "cache.h"
-#include "mfma_common.h"
+#include "cache_cut.h"
 
 namespace ssa {
 namespace {
 
-enum { BF = 0, F8 = 1, I8 = 2 };
-
-// What one sequence has: its new tokens' rows, the keys before them and in all, and the parts of `chunk` keys.
-struct CacheSeq {
-  int q0, n, before, len;
-};
-__device__ __forceinline__ CacheSeq cache_seq(const CacheAttnP& p, int b) {
-  CacheSeq s;
-  s.q0 = min(max(p.cu[b], 0), p.T);
-  const int n = max(min(p.cu[b + 1], p.T) - s.q0, 0), lens = max(p.lens[b], 0);
-  s.n = min(n, p.max_new);
-  s.before = max(lens - n, 0);
-  s.len = (int)min((int64_t)lens, (int64_t)p.c.max_pages << p.c.shift);  // keys that the table has a place for
-  return s;
-}
-__device__ __forceinline__ int parts_of(const CacheSeq& s, int chunk) { return s.n > 0 ? (s.len > 0 ? (s.len - 1) / chunk + 1 : 1) : 0; }
-
-__device__ __forceinline__ int scan64(int x) {  // inclusive prefix sums over the wavefront
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-__device__ __forceinline__ CacheSeq lane_seq(const CacheAttnP& p, int b) {
-  CacheSeq s = cache_seq(p, min(b, p.c.n_seq - 1));
-  if (b >= p.c.n_seq) s.n = s.len = 0;
-  return s;
-}
-// keys of a part: enough parts to fill the chip (`p.parts` of them over all sequences), not shorter than p.least
-__device__ __forceinline__ int chunk_of(const CacheAttnP& p) {
-  int64_t total = 0;
-  for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
-    const CacheSeq s = lane_seq(p, b0 + (int)(threadIdx.x & 63));
-    // (in units of 128 keys: the sum of 64 sequences of 2^31 keys fits)
-    total += __builtin_amdgcn_readlane(scan64(s.n > 0 ? (s.len >> 7) + 1 : 0), 63);
-  }
-  return (int)max((int64_t)p.least, min((total + p.parts - 1) / p.parts * 128, (int64_t)0x7fffff80));
-}
-// the sequence of slot `slot`, and its part there; b = -1: fewer slots than that
-struct Slot {
-  CacheSeq s;
-  int b, part, parts;
-};
-__device__ __forceinline__ Slot find_slot(const CacheAttnP& p, int chunk, int slot) {
-  const int lane = threadIdx.x & 63;
-  Slot f;
-  f.b = -1;
-  for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
-    const CacheSeq s = lane_seq(p, b0 + lane);
-    const int mine = parts_of(s, chunk), upto = scan64(mine), all = __builtin_amdgcn_readlane(upto, 63);
-    if (slot >= all) {
-      slot -= all;
-      continue;
-    }
-    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > slot));
-    f.s.q0 = __builtin_amdgcn_readlane(s.q0, l);
-    f.s.n = __builtin_amdgcn_readlane(s.n, l);
-    f.s.before = __builtin_amdgcn_readlane(s.before, l);
-    f.s.len = __builtin_amdgcn_readlane(s.len, l);
-    f.b = b0 + l;
-    f.parts = __builtin_amdgcn_readlane(mine, l);
-    f.part = slot - (__builtin_amdgcn_readlane(upto, l) - f.parts);
-    return f;
-  }
-  return f;
-}
-
 // two bf16 of one register's 16-bit halves
 __device__ __forceinline__ uint32_t lo_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t hi_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-// two 8-bit codes (bytes 2 HI and 2 HI + 1) as packed bf16, exactly
-template <int FMT, bool HI>
-__device__ __forceinline__ uint32_t two_codes(uint32_t x) {
-  if (FMT == F8) {
-    union { bf16x2 v; uint32_t u; } o;
-    o.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, HI);
-    return o.u;
-  }
-  return pack2_bf16((float)(int8_t)(x >> (HI ? 16 : 0)), (float)(int8_t)(x >> (HI ? 24 : 8)));
-}
-
 template <int FMT, int D>
 struct CacheTile {
   static constexpr int E = FMT == BF ? 2 : 1, ROW_B = D * E, KS = D / 16, NB = D / 32;
@@ -109,22 +27,20 @@ struct CacheTile {
   static constexpr int VR = VW == 8 ? 2 : 1;  // registers
 };
 
-template <int FMT, int D, int NQ>
+template <int FMT, int D>
 __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem) {
   using T = CacheTile<FMT, D>;
   constexpr int KS = T::KS, NB = T::NB, ROW_B = T::ROW_B;
   const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // row groups of one part next to each other on one XCD: all but the first find its keys in that XCD's L2
-  const int idx = blockIdx.x >> 3, unit = idx / p.groups * 8 + (int)(blockIdx.x & 7), rg = idx % p.groups;
-  const int slot = unit / p.c.HK, hk = unit - slot * p.c.HK;
+  const int slot = blockIdx.x / p.c.HK, hk = blockIdx.x - slot * p.c.HK;
   if (slot >= p.slots) return;
-  const int chunk = chunk_of(p);
-  const Slot f = find_slot(p, chunk, slot);
+  const Cut cut(p);
+  const int chunk = cut.chunk;
+  const Slot f = cut.find(slot);
   if (f.b < 0) return;
   const CacheSeq s = f.s;
-  const int rows = s.n * p.G, row0 = 32 * NQ * rg;
-  if (row0 >= rows) return;
+  const int rows = s.n * p.G;  // up to 32
   const int begin = f.part * chunk, end = begin + min(chunk, s.len - begin);
   const int shift = p.c.shift;
 
@@ -133,17 +49,15 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
   const int last_entry = (end - 1) >> shift;
   auto entries = [&](int from) {
     const int e = from + lane;
-    const int page = e <= last_entry ? line[e] : -1;
-    return page >= 0 && page < p.c.n_pages ? page : -1;
+    return e <= last_entry ? line[e] : -1;  // (looked at when it is used, so that nothing waits for it here)
   };
   int window = (begin + 32 * w) >> shift;
   int win = entries(window), win_next = entries(window + 64);
 
-  bf16x8 qf[NQ][KS];
-  uint64_t bits[NQ];
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const int R = min(row0 + 32 * q + r, rows - 1), tok = R / p.G, h = hk * p.G + R - tok * p.G;
+  bf16x8 qf[KS];
+  uint64_t bits;
+  {
+    const int R = min(r, rows - 1), tok = R / p.G, h = hk * p.G + R - tok * p.G;
     const uint16_t* Q = (const uint16_t*)p.Q + (int64_t)(s.q0 + tok) * p.q_st + (int64_t)h * p.q_sh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -154,9 +68,9 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
       const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.u[e] ^= flip;
-      qf[q][ks] = x.v;
+      qf[ks] = x.v;
     }
-    bits[q] = p.tree ? p.tree[s.q0 + tok] : ~(~(uint64_t)1 << tok);
+    bits = p.tree ? p.tree[s.q0 + tok] : ~(~(uint64_t)1 << tok);
   }
   // (a factor of 0 would make NaN of a masked score)
   const float c1 = fmaxf(fabsf(p.scale) * LOG2E, 0x1p-120f);
@@ -176,9 +90,10 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
     int64_t rk = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int pos = k0 + 8 * g, page = __builtin_amdgcn_readlane(win, (pos >> shift) - window);
-      if (page < 0) there &= ~(0xffu << (8 * g));
-      row_of[g] = cache_row(max(page, 0), shift, p.c.HK, hk, pos);
+      const int pos = k0 + 8 * g, entry = __builtin_amdgcn_readlane(win, (pos >> shift) - window);
+      const bool is = (uint32_t)entry < (uint32_t)p.c.n_pages;
+      if (!is) there &= ~(0xffu << (8 * g));
+      row_of[g] = cache_row(is ? entry : 0, shift, p.c.HK, hk, pos);
       if (r >> 3 == g) rk = row_of[g];
     }
     live_next = there;
@@ -211,17 +126,12 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
     }
   };
 
-  f32x16 acc[NQ][NB];
-  float m[NQ], l[NQ];
+  f32x16 acc[NB];
+  float m = -1e30f, l = 0.f;
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    m[q] = -1e30f;
-    l[q] = 0.f;
+  for (int e = 0; e < NB; ++e)
 #pragma unroll
-    for (int e = 0; e < NB; ++e)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[q][e][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) acc[e][v] = 0.f;
   int k0 = begin + 32 * w;
   if (k0 < end) {
     locate(k0);
@@ -229,11 +139,9 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
   }
   for (; k0 < end; k0 += 128) {
     live = live_next;
-    f32x16 sa[NQ];
+    f32x16 sa;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sa[q][v] = 0.f;
+      for (int v = 0; v < 16; ++v) sa[v] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       union { u32x4 u; bf16x8 v; } k;
@@ -247,8 +155,7 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
           k.u[2 * h + 1] = two_codes<FMT, true>(x);
         }
       }
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) sa[q] = mfma(k.v, qf[q][ks], sa[q]);
+      sa = mfma(k.v, qf[ks], sa);
     }
     float kc[16];  // what makes a score of a product, in base-2 units
 #pragma unroll
@@ -257,38 +164,37 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
     // all keys are there and none is a new token: nothing to mask
     const bool plain = live == ~0u && k0 + 32 <= s.before;
     if (more) locate(k0 + 128);  // K of the next block starts on its way
-    bf16x8 pf[NQ][2];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
+    bf16x8 pf[2];
+    {
       uint32_t seen = ~0u;  // keys of the block that this lane's row sees, from the half-wave's first on
 #pragma unroll
-      for (int v = 0; v < 16; ++v) sa[q][v] *= kc[v];
+      for (int v = 0; v < 16; ++v) sa[v] *= kc[v];
       if (!plain) {
         const int nb = s.before - k0;
         const uint32_t old = nb >= 32 ? ~0u : nb > 0 ? (1u << nb) - 1u : 0u;
-        const uint32_t fresh = nb >= 32 ? 0u : nb >= 0 ? (uint32_t)(bits[q] << nb) : nb > -64 ? (uint32_t)(bits[q] >> -nb) : 0u;
+        const uint32_t fresh = nb >= 32 ? 0u : nb >= 0 ? (uint32_t)(bits << nb) : nb > -64 ? (uint32_t)(bits >> -nb) : 0u;
         seen = (live & (old | fresh)) >> (4 * hl);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sa[q][v] = seen >> (8 * (v >> 2) + (v & 3)) & 1u ? sa[q][v] : -INFINITY;
+        for (int v = 0; v < 16; ++v) sa[v] = seen >> (8 * (v >> 2) + (v & 3)) & 1u ? sa[v] : -INFINITY;
       }
       float rmax = -INFINITY;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) rmax = fmaxf(rmax, sa[q][v]);
+      for (int v = 0; v < 16; ++v) rmax = fmaxf(rmax, sa[v]);
       rmax = half_max(rmax);
       // the maximum is raised when exceeded by more than 2^8: probabilities stay below that
-      if (__builtin_amdgcn_ballot_w64(rmax > m[q] + 8.f) != 0) {
-        const float mn = fmaxf(m[q], rmax), alpha = fast_exp2(m[q] - mn);
-        m[q] = mn;
-        l[q] *= alpha;
+      if (__builtin_amdgcn_ballot_w64(rmax > m + 8.f) != 0) {
+        const float mn = fmaxf(m, rmax), alpha = fast_exp2(m - mn);
+        m = mn;
+        l *= alpha;
 #pragma unroll
         for (int e = 0; e < NB; ++e)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) acc[q][e][v] *= alpha;
+          for (int v = 0; v < 16; ++v) acc[e][v] *= alpha;
       }
       float pr[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) pr[v] = fast_exp2(sa[q][v] - m[q]);
-      l[q] += sum16(pr);
+      for (int v = 0; v < 16; ++v) pr[v] = fast_exp2(sa[v] - m);
+      l += sum16(pr);
       if (FMT != BF) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) pr[v] *= __uint_as_float(vs4[v >> 2][v & 3]);
@@ -297,8 +203,8 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
 #pragma unroll
         for (int v = 0; v < 16; ++v) pr[v] = seen >> (8 * (v >> 2) + (v & 3)) & 1u ? pr[v] : 0.f;
       }
-      pf[q][0] = pack8(&pr[0]);
-      pf[q][1] = pack8(&pr[8]);
+      pf[0] = pack8(&pr[0]);
+      pf[1] = pack8(&pr[8]);
     }
     if (live != ~0u) {  // ... and any code
 #pragma unroll
@@ -333,8 +239,7 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
       for (int e = 0; e < NB; ++e) {
         union { u32x4 u; bf16x8 v; } a;
         a.u = vf[e];
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[q][e] = mfma(a.v, pf[q][t], acc[q][e]);
+        acc[e] = mfma(a.v, pf[t], acc[e]);
       }
     }
     if (more) load_v();
@@ -344,13 +249,12 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
   // NB (8 (v / 4) + 4 hl + v % 4) + e: wavefront w adds up registers 4 w .. 4 w + 3, 4 NB neighbouring columns of each row.
   float* ml = (float*)smem;               // [wavefront][maximum, sum][32]
   float4* part = (float4*)(smem + 1024);  // [wavefront][e][quarter][lane]
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    l[q] = half_sum(l[q]);
+  {
+    l = half_sum(l);
     __syncthreads();
     if (hl == 0) {
-      ml[64 * w + r] = m[q];
-      ml[64 * w + 32 + r] = l[q];
+      ml[64 * w + r] = m;
+      ml[64 * w + 32 + r] = l;
     }
     __syncthreads();
     float mg = -1e30f, sum = 0.f;
@@ -358,12 +262,12 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
     for (int x = 0; x < 4; ++x) mg = fmaxf(mg, ml[64 * x + r]);
 #pragma unroll
     for (int x = 0; x < 4; ++x) sum = fmaf(fast_exp2(ml[64 * x + r] - mg), ml[64 * x + 32 + r], sum);
-    const float mine = fast_exp2(m[q] - mg);
+    const float mine = fast_exp2(m - mg);
 #pragma unroll
     for (int e = 0; e < NB; ++e)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        part[((w * NB + e) * 4 + g) * 64 + lane] = make_float4(acc[q][e][4 * g] * mine, acc[q][e][4 * g + 1] * mine, acc[q][e][4 * g + 2] * mine, acc[q][e][4 * g + 3] * mine);
+        part[((w * NB + e) * 4 + g) * 64 + lane] = make_float4(acc[e][4 * g] * mine, acc[e][4 * g + 1] * mine, acc[e][4 * g + 2] * mine, acc[e][4 * g + 3] * mine);
     __syncthreads();
     float o[4 * NB];
 #pragma unroll
@@ -376,8 +280,8 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
       }
       o[e] = x.x; o[NB + e] = x.y; o[2 * NB + e] = x.z; o[3 * NB + e] = x.w;
     }
-    const int R = row0 + 32 * q + r, col = NB * (8 * w + 4 * hl);
-    if (R >= rows) continue;  // (no barrier is left out: `continue` leaves a lane's stores only)
+    const int R = r, col = NB * (8 * w + 4 * hl);
+    if (R >= rows) return;
     if (f.parts == 1) {
       const int tok = R / p.G, h = hk * p.G + R - tok * p.G;
       const float inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
@@ -397,71 +301,111 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
   }
 }
 
-template <int FMT, int D, int NQ>
-__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnP p) {
+template <int FMT, int D>
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnP p) {
   __shared__ __attribute__((aligned(1024))) char smem[1024 + 4 * 32 * D * 4];
-  cache_attn_part<FMT, D, NQ>(p, smem);
+  cache_attn_part<FMT, D>(p, smem);
 }
 
-// Rows of sequences in more than one part: a wavefront per token and head, the parts in order.
-template <int D>
+// Rows of sequences in more than one part: W wavefronts per token and head.  D / 4 lanes take a part's columns, each of 64 W / (D / 4) groups of lanes
+// every so many parts, four at a time on their way, with a running maximum; then the groups are joined, in order.  Bound by
+// the way of a few loads that follow each other (offsets, then the parts).
+template <int D, int W>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnP p) {
-  constexpr int C = D / 64;  // columns of a lane
-  const int lane = threadIdx.x & 63;
-  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), t = unit / p.H, h = unit - t * p.H;
+  constexpr int LANES = D / 4, GROUPS = 64 / LANES, STRIDE = W * GROUPS;
+  const int lane = threadIdx.x & 63, c = lane % LANES, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave, t = unit / p.H, h = unit - t * p.H;
   if (t >= p.T) return;
-  const int chunk = chunk_of(p);
-  const int b = packed_owner(p.cu, p.c.n_seq, t);
-  if (b < 0) return;
-  const CacheSeq s = cache_seq(p, b);
-  const int parts = parts_of(s, chunk), tok = t - s.q0;
-  if (parts < 2 || tok >= s.n) return;
-  int slot = 0;  // the sequence's first
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int i = b0 + lane;
-    slot += __builtin_amdgcn_readlane(scan64(i < b ? parts_of(cache_seq(p, i), chunk) : 0), 63);
-  }
-  const int hk = h / p.G, R = tok * p.G + h - hk * p.G;
+  const Cut cut(p);
+  const Slot f = cut.owner(t);
+  if (f.b < 0 || f.parts < 2) return;
+  const int parts = f.parts, hk = h / p.G, R = (t - f.s.q0) * p.G + h - hk * p.G;
   const float* ws = (const float*)p.ws;
-  const int64_t first = ((int64_t)slot * p.c.HK + hk) * p.max_rows + R, step = (int64_t)p.c.HK * p.max_rows;
-  float mg = -1e30f;
-  for (int x = lane; x < parts; x += 64) mg = fmaxf(mg, ws[p.ml_at + 2 * (first + x * step)]);
+  const int64_t first = ((int64_t)f.part * p.c.HK + hk) * p.max_rows + R, step = (int64_t)p.c.HK * p.max_rows;
+  const float2* ml = (const float2*)(ws + p.ml_at) + first;
+  float m = -1e30f, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int x0 = (W == 4 ? wave * GROUPS : 0) + lane / LANES; x0 < parts; x0 += 4 * STRIDE) {
+    float4 o[4];
+    float2 s[4];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) mg = fmaxf(mg, __shfl_xor(mg, o));
-  float sum = 0.f, acc[C];
+    for (int i = 0; i < 4; ++i) {
+      const int x = min(x0 + i * STRIDE, parts - 1);
+      s[i] = ml[x * step];
+      o[i] = *(const float4*)(ws + (first + x * step) * D + 4 * c);
+    }
+    float mn = m;
 #pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = 0.f;
-  for (int x = 0; x < parts; ++x) {
-    const int64_t at = first + x * step;
-    const float2 ml = *(const float2*)(ws + p.ml_at + 2 * at);
-    const float a = fast_exp2(ml.x - mg);
-    sum = fmaf(a, ml.y, sum);
+    for (int i = 0; i < 4; ++i) mn = fmaxf(mn, s[i].x);
+    const float old = fast_exp2(m - mn);
+    m = mn;
+    sum *= old;
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] = fmaf(a, ws[at * D + C * lane + c], acc[c]);
+    for (int j = 0; j < 4; ++j) acc[j] *= old;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (x0 + i * STRIDE >= parts) break;
+      const float a = fast_exp2(s[i].x - m);
+      sum = fmaf(a, s[i].y, sum);
+      acc[0] = fmaf(a, o[i].x, acc[0]);
+      acc[1] = fmaf(a, o[i].y, acc[1]);
+      acc[2] = fmaf(a, o[i].z, acc[2]);
+      acc[3] = fmaf(a, o[i].w, acc[3]);
+    }
   }
+  auto join = [&](float m1, float sum1, const float (&acc1)[4]) {
+    const float mn = fmaxf(m, m1), a0 = fast_exp2(m - mn), a1 = fast_exp2(m1 - mn);
+    m = mn;
+    sum = fmaf(a1, sum1, a0 * sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = fmaf(a1, acc1[j], a0 * acc[j]);
+  };
+#pragma unroll
+  for (int o = LANES; o < 64; o <<= 1) {
+    float other[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) other[j] = __shfl_down(acc[j], o);  // (the first group's lanes are what counts)
+    join(__shfl_down(m, o), __shfl_down(sum, o), other);
+  }
+  if (W == 4) {
+    __shared__ float4 parts_of_waves[4][64];
+    __shared__ float2 ml_of_waves[4];
+    parts_of_waves[wave][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (lane == 0) ml_of_waves[wave] = make_float2(m, sum);
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int x = 1; x < 4; ++x) {
+      const float4 y = parts_of_waves[x][lane];
+      const float other[4] = {y.x, y.y, y.z, y.w};
+      join(ml_of_waves[x].x, ml_of_waves[x].y, other);
+    }
+  }
+  if (lane >= LANES) return;
   const float inv = sum > 0.f ? 1.f / sum : sum;
-  uint16_t* y = (uint16_t*)p.Y + (int64_t)t * p.y_st + (int64_t)h * p.y_sh + C * lane;
-  if (C == 2) *(uint32_t*)y = pack2_bf16(acc[0] * inv, acc[C - 1] * inv);
-  else *y = f2bf(acc[0] * inv);
-  if (p.lse && lane == 0) p.lse[(int64_t)h * p.T + t] = sum == 0.f ? -INFINITY : (mg + log2f(sum)) * LN2;
+  *(uint2*)((uint16_t*)p.Y + (int64_t)t * p.y_st + (int64_t)h * p.y_sh + 4 * c) = pack4_bf16(acc[0], acc[1], acc[2], acc[3], inv);
+  if (p.lse && lane == 0) p.lse[(int64_t)h * p.T + t] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
 }
 
 template <int FMT, int D>
 void launch(const CacheAttnP& p, int blocks, hipStream_t st) {
-  if (p.max_rows <= 32) cache_attn_kernel<FMT, D, 1><<<blocks, 256, 0, st>>>(p);
-  else cache_attn_kernel<FMT, D, 2><<<blocks, 256, 0, st>>>(p);
+  cache_attn_kernel<FMT, D><<<blocks, 256, 0, st>>>(p);
+}
+template <int D>
+void launch_join(const CacheAttnP& p, hipStream_t st) {
+  const int64_t units = (int64_t)p.T * p.H;
+  if (units <= 1024) cache_join_kernel<D, 4><<<(int)units, 256, 0, st>>>(p);
+  else cache_join_kernel<D, 1><<<(int)((units + 3) / 4), 256, 0, st>>>(p);
 }
 
 // How the work is cut: from the descriptors alone.
 void cut(CacheAttnP& p) {
   p.max_rows = p.max_new * p.G;
-  p.groups = p.max_rows <= 32 ? 1 : (p.max_rows + 63) / 64;
+  p.groups = (p.max_rows + 127) / 128;
   const int64_t most = (int64_t)p.c.max_pages << p.c.shift;  // keys of a sequence
-  // two work-groups to a compute unit (one with 64 rows a wavefront); a context that fits 512 keys is one part
-  const int64_t want = (p.max_rows <= 32 ? 512 : 256) / ((int64_t)p.c.HK * p.groups);
+  const int64_t want = 512 / ((int64_t)p.c.HK * p.groups);   // two work-groups to a compute unit
   p.parts = (int)(want > 1 ? want : 1);
-  p.least = most <= 512 ? 512 : 256;
-  p.slots = p.parts + p.c.n_seq;
+  p.least = most <= 512 ? 512 : 256;  // a context that fits 512 keys is one part
+  p.slots = 2 * p.parts + p.c.n_seq;
   p.ml_at = (int64_t)p.slots * p.c.HK * p.max_rows * p.c.D;
 }
 bool one_part(const CacheAttnP& p) { return ((int64_t)p.c.max_pages << p.c.shift) <= p.least; }
@@ -477,19 +421,22 @@ size_t cache_attn_bytes(const CacheAttnP& q) {
 hipError_t launch_cache_attn(const CacheAttnP& q, hipStream_t st) {
   CacheAttnP p = q;
   cut(p);
-  const int blocks = (int)((((int64_t)p.slots * p.c.HK + 7) / 8) * 8 * p.groups);
   auto by_size = [&](auto fmt) {
-    if (p.c.D == 64) launch<fmt(), 64>(p, blocks, st);
-    else launch<fmt(), 128>(p, blocks, st);
+    if (p.c.D == 64) launch<fmt(), 64>(p, p.slots * p.c.HK, st);
+    else launch<fmt(), 128>(p, p.slots * p.c.HK, st);
   };
-  if (p.c.format == BF) by_size(std::integral_constant<int, BF>{});
-  else if (p.c.format == F8) by_size(std::integral_constant<int, F8>{});
-  else by_size(std::integral_constant<int, I8>{});
-  const hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (p.max_rows > 32) {
+    e = launch_cache_attn_rows(p, (int)((((int64_t)p.slots * p.c.HK + 7) / 8) * 8 * p.groups), st);
+  } else {
+    if (p.c.format == BF) by_size(std::integral_constant<int, BF>{});
+    else if (p.c.format == F8) by_size(std::integral_constant<int, F8>{});
+    else by_size(std::integral_constant<int, I8>{});
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || one_part(p)) return e;
-  const int units = (int)(((int64_t)p.T * p.H + 3) / 4);
-  if (p.c.D == 64) cache_join_kernel<64><<<units, 256, 0, st>>>(p);
-  else cache_join_kernel<128><<<units, 256, 0, st>>>(p);
+  if (p.c.D == 64) launch_join<64>(p, st);
+  else launch_join<128>(p, st);
   return hipGetLastError();
 }
 

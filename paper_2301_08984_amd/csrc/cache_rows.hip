@@ -1,7 +1,7 @@
 // Rows into the paged cache and out of it (include/ss_cache.h): quantised as they are written, and read back.
 //
-// A row of D values is D / 8 lanes with 16 bytes each, so a wavefront takes 4 rows (D = 128) or 8 at a time, of one token:
-// the K rows of its heads, then the V rows.  The largest magnitude goes round the row's lanes, every lane converts its
+// A row of D values is D / 8 lanes with 16 bytes each, so a wavefront takes 4 rows (D = 128) or 8, of one token (of
+// its K rows, one a head, and V rows behind them).  The largest magnitude goes round the row's lanes, every lane converts its
 // own eight values.  Bound by memory: 4 D bytes in and 2 D + 8 out for a token and head, or the reverse.
 #include "cache.h"
 #include "mfma_common.h"
@@ -16,35 +16,55 @@ __device__ inline float fp8_scale(float most) {
   return exp2_int(max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -126));
 }
 
-// where a token's rows lie in the cache: its sequence's page, and the place in the pages' rows of head 0
+// What a wavefront does: rows `first` .. of token t, and where they lie in the cache.
 struct Place {
   int page;  // -1: none
   int64_t pos;
 };
-__device__ inline Place place_of(const CacheRowsP& p, int t, int b) {
-  Place a;
-  a.pos = (int64_t)t - p.cu[b] + (p.start ? p.start[b] : 0);
-  a.page = cache_page(p.c.table, p.c.n_pages, p.c.shift, p.c.max_pages, b, a.pos);
-  return a;
+// The token's sequence (b = -1: none) and place: the offsets and starts of 64 sequences are asked for at once, so that the table's
+// entry, which they name, is the second load in a row and not the third.
+__device__ __forceinline__ int place_of(const CacheRowsP& p, int t, Place& at) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
+    const int i = min(b0 + lane, p.c.n_seq - 1);
+    const int from = p.cu[i], to = p.cu[i + 1], start = p.start ? p.start[i] : 0;
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.n_seq && from <= t && t < to);
+    if (!hit) continue;
+    const int l = 63 - __builtin_clzll(hit);
+    at.pos = (int64_t)t - __builtin_amdgcn_readlane(from, l) + __builtin_amdgcn_readlane(start, l);
+    at.page = cache_page(p.c.table, p.c.n_pages, p.c.shift, p.c.max_pages, b0 + l, at.pos);
+    return b0 + l;
+  }
+  return -1;
+}
+// A wavefront's part of the launch: every p.groups-th ROWS of a token's 2 HK rows, from row r0 on.
+template <int ROWS>
+__device__ __forceinline__ bool rows_of(const CacheRowsP& p, int& t, int& r0) {
+  const int u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  t = u / p.groups;
+  r0 = (u - t * p.groups) * ROWS;
+  return t < p.T;
 }
 
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheRowsP p) {
   constexpr int LANES = D / 8, ROWS = 64 / LANES;
-  const int lane = threadIdx.x & 63, c = lane % LANES;
-  const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (t >= p.T) return;
-  const int b = packed_owner(p.cu, p.c.n_seq, t);
-  if (b < 0) return;
-  const Place at = place_of(p, t, b);
-  if (at.page < 0) return;
-  const int HK = p.c.HK;
-  for (int r0 = 0; r0 < 2 * HK; r0 += ROWS) {
-    const int r = r0 + lane / LANES;
-    if (r >= 2 * HK) break;  // (whole rows of lanes leave)
+  const int lane = threadIdx.x & 63, c = lane % LANES, HK = p.c.HK;
+  int t, r0;
+  if (!rows_of<ROWS>(p, t, r0)) return;
+  auto load = [&](int r) {
+    const bool v = r >= HK;
+    return r < 2 * HK ? *(const u32x4*)((const uint16_t*)(v ? p.V : p.K) + t * p.st + (v ? r - HK : r) * p.sh + 8 * c) : u32x4{0, 0, 0, 0};
+  };
+  int r = r0 + lane / LANES;
+  u32x4 next = load(r);
+  Place at;
+  if (place_of(p, t, at) < 0 || at.page < 0) return;
+  for (; r < 2 * HK; r += p.groups * ROWS) {  // (whole rows of lanes leave)
+    const u32x4 x = next;
+    next = load(r + p.groups * ROWS);
     const bool v = r >= HK;
     const int h = v ? r - HK : r;
-    const u32x4 x = *(const u32x4*)((const uint16_t*)(v ? p.V : p.K) + t * p.st + h * p.sh + 8 * c);
     const int64_t row = cache_row(at.page, p.c.shift, HK, h, at.pos);
     if (FMT == 0) {
       *(u32x4*)((uint16_t*)(v ? p.c.vc : p.c.kc) + row * D + 8 * c) = x;
@@ -87,16 +107,13 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheRowsP p) {
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRowsP p) {
   constexpr int LANES = D / 8, ROWS = 64 / LANES;
-  const int lane = threadIdx.x & 63, c = lane % LANES;
-  const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (t >= p.T) return;
-  const int b = packed_owner(p.cu, p.c.n_seq, t);
-  if (b < 0) return;
-  const Place at = place_of(p, t, b);
-  const int HK = p.c.HK;
-  for (int r0 = 0; r0 < 2 * HK; r0 += ROWS) {
-    const int r = r0 + lane / LANES;
-    if (r >= 2 * HK) break;
+  const int lane = threadIdx.x & 63, c = lane % LANES, HK = p.c.HK;
+  int t, r0;
+  if (!rows_of<ROWS>(p, t, r0)) return;
+  Place at;
+  if (place_of(p, t, at) < 0) return;
+#pragma unroll 2
+  for (int r = r0 + lane / LANES; r < 2 * HK; r += p.groups * ROWS) {
     const bool v = r >= HK;
     const int h = v ? r - HK : r;
     u32x4 x = {0, 0, 0, 0};
@@ -139,13 +156,25 @@ hipError_t with_format(const CacheP& c, F&& f) {
   return hipGetLastError();
 }
 
+// Wavefronts of a token, and work-groups of the launch: one wavefront for four (eight) rows while those are few, one for a token's rows
+// where there are tokens enough.  READ_TIMES
+int cut(CacheRowsP& p) {
+  const int rows = 512 / p.c.D;
+  p.groups = p.T < 4096 ? (2 * p.c.HK + rows - 1) / rows : 1;
+  return (int)(((int64_t)p.T * p.groups + 3) / 4);
+}
+
 }  // namespace
 
-hipError_t launch_cache_write(const CacheRowsP& p, hipStream_t st) {
-  return with_format(p.c, [&](auto fmt, auto d) { cache_write_kernel<fmt(), d()><<<(p.T + 3) / 4, 256, 0, st>>>(p); });
+hipError_t launch_cache_write(const CacheRowsP& q, hipStream_t st) {
+  CacheRowsP p = q;
+  const int blocks = cut(p);
+  return with_format(p.c, [&](auto fmt, auto d) { cache_write_kernel<fmt(), d()><<<blocks, 256, 0, st>>>(p); });
 }
-hipError_t launch_cache_read(const CacheRowsP& p, hipStream_t st) {
-  return with_format(p.c, [&](auto fmt, auto d) { cache_read_kernel<fmt(), d()><<<(p.T + 3) / 4, 256, 0, st>>>(p); });
+hipError_t launch_cache_read(const CacheRowsP& q, hipStream_t st) {
+  CacheRowsP p = q;
+  const int blocks = cut(p);
+  return with_format(p.c, [&](auto fmt, auto d) { cache_read_kernel<fmt(), d()><<<blocks, 256, 0, st>>>(p); });
 }
 
 }  // namespace ssa
