@@ -51,9 +51,10 @@ struct CacheAttnP {
   float scale;
   int T, H, G, max_new;
   char* ws;
-  // how the work is cut (cache_attn.hip): rows of a sequence and key head at most, groups of 128 of them, parts to aim at, slots for
-  // parts, the shortest part, and where in the workspace, in floats, the parts' maxima and sums begin
-  int max_rows, groups, parts, slots, least;
+  // how the work is cut (cache_cut.h): rows of a sequence and key head at most, and of a part; pieces, the shortest one, whether every run
+  // is one; and where in the workspace, in floats, the parts' maxima and sums begin
+  int max_rows, part_rows, pieces, least;
+  bool whole;
   int64_t ml_at;
 };
 size_t cache_attn_bytes(const CacheAttnP& p);

@@ -35,8 +35,9 @@ int validate(const ss_cache_desc* d, const ss_cache_attn_desc* a) {
   if (a->T < 1 || a->H < 1 || a->H % d->HK || a->max_new < 1 || !std::isfinite(a->scale)) return SS_ERR_BAD_SHAPE;
   if (bad_stride(a->q_stride_t, a->q_stride_h, d->D) || bad_stride(a->y_stride_t, a->y_stride_h, d->D)) return SS_ERR_BAD_SHAPE;
   if (a->max_new > 64 || a->H > 65535 || (int64_t)a->T * a->H >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
-  // (work-groups are counted in 31 bits)
-  if ((int64_t)(1032 + d->n_seq) * d->HK * ((a->max_new * (a->H / d->HK) + 127) / 128) >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
+  // (all sequences' keys, 64 at a time, once for every 128 rows, and work-groups are counted in 31 bits)
+  const int64_t runs = (int64_t)d->n_seq * ((a->max_new * (a->H / d->HK) + 127) / 128);
+  if (runs * ((((int64_t)d->max_pages * d->page) >> 6) + 1) >= (int64_t)1 << 30 || runs * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
 

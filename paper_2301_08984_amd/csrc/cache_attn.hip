@@ -2,10 +2,9 @@
 //
 // Bound by reading the cache: 4 D bytes (2 D + 8 in 8 bits) a key and head for 4 D flops a row, so a key is read once for all rows that see
 // it, the new tokens of a sequence times the G query heads of a key head, here up to 32 (more: cache_attn_rows.hip), and goes from memory into
-// registers: nothing passes through LDS until the end.  The keys of all sequences are cut into parts of about equal length, so that a long
-// sequence does not keep the chip waiting; the four wavefronts of a work-group take every fourth block of 32 keys of a part each, with a
-// running maximum and sum, and are joined through LDS.  A sequence in one part is finished there; the others' parts are joined by
-// a second launch.
+// registers: nothing passes through LDS until the end.  The keys of all sequences are dealt out to the work-groups in equal pieces (cache_cut.h);
+// the four wavefronts of a work-group take every fourth block of 32 keys of a piece each, with a running maximum and sum, and are
+// joined through LDS.  A sequence within a piece is finished there; the parts of the others are joined by a second launch.
 //
 // Scores: S^T = K Q^T, a lane holding 16 (D = 128: of the row's 128) columns of its key, as they come; 8-bit codes become bf16
 // exactly, and the key's scale multiplies the fp32 score.  O^T += V^T P^T: a lane holds D / 32 neighbouring columns of eight keys, which byte permutes turn
@@ -27,22 +26,17 @@ struct CacheTile {
   static constexpr int VR = VW == 8 ? 2 : 1;  // registers
 };
 
+// One run (or part of one) of a piece: keys begin .. end of it; `all`: the whole of it.
 template <int FMT, int D>
-__device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem) {
+__device__ __forceinline__ void cache_attn_run(const CacheAttnP& p, char* smem, const Run& f, int hk, int begin, int end, bool all, int slot) {
   using T = CacheTile<FMT, D>;
   constexpr int KS = T::KS, NB = T::NB, ROW_B = T::ROW_B;
-  const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
+  int lane = threadIdx.x & 63;
+  asm("" : "+v"(lane));  // (what follows from it is formed anew for every run: kept over the loop, it spills)
+  const int r = lane & 31, hl = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int slot = blockIdx.x / p.c.HK, hk = blockIdx.x - slot * p.c.HK;
-  if (slot >= p.slots) return;
-  const Cut cut(p);
-  const int chunk = cut.chunk;
-  const Slot f = cut.find(slot);
-  if (f.b < 0) return;
   const CacheSeq s = f.s;
-  const int rows = s.n * p.G;  // up to 32
-  const int begin = f.part * chunk, end = begin + min(chunk, s.len - begin);
-  const int shift = p.c.shift;
+  const int rows = s.n * p.G, shift = p.c.shift;  // up to 32 rows
 
   // pages of the part: a lane an entry, 64 of them and the 64 behind them
   const int32_t* line = p.c.table + (int64_t)f.b * p.c.max_pages;
@@ -249,62 +243,67 @@ __device__ __forceinline__ void cache_attn_part(const CacheAttnP& p, char* smem)
   // NB (8 (v / 4) + 4 hl + v % 4) + e: wavefront w adds up registers 4 w .. 4 w + 3, 4 NB neighbouring columns of each row.
   float* ml = (float*)smem;               // [wavefront][maximum, sum][32]
   float4* part = (float4*)(smem + 1024);  // [wavefront][e][quarter][lane]
-  {
-    l = half_sum(l);
-    __syncthreads();
-    if (hl == 0) {
-      ml[64 * w + r] = m;
-      ml[64 * w + 32 + r] = l;
+  l = half_sum(l);
+  __syncthreads();
+  if (hl == 0) {
+    ml[64 * w + r] = m;
+    ml[64 * w + 32 + r] = l;
+  }
+  __syncthreads();
+  float mg = -1e30f, sum = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) mg = fmaxf(mg, ml[64 * x + r]);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) sum = fmaf(fast_exp2(ml[64 * x + r] - mg), ml[64 * x + 32 + r], sum);
+  const float mine = fast_exp2(m - mg);
+#pragma unroll
+  for (int e = 0; e < NB; ++e)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      part[((w * NB + e) * 4 + g) * 64 + lane] = make_float4(acc[e][4 * g] * mine, acc[e][4 * g + 1] * mine, acc[e][4 * g + 2] * mine, acc[e][4 * g + 3] * mine);
+  __syncthreads();
+  float o[4 * NB];
+#pragma unroll
+  for (int e = 0; e < NB; ++e) {
+    float4 x = part[((0 * NB + e) * 4 + w) * 64 + lane];
+#pragma unroll
+    for (int y = 1; y < 4; ++y) {
+      const float4 z = part[((y * NB + e) * 4 + w) * 64 + lane];
+      x.x += z.x; x.y += z.y; x.z += z.z; x.w += z.w;
     }
-    __syncthreads();
-    float mg = -1e30f, sum = 0.f;
+    o[e] = x.x; o[NB + e] = x.y; o[2 * NB + e] = x.z; o[3 * NB + e] = x.w;
+  }
+  const int R = r, col = NB * (8 * w + 4 * hl);
+  if (R >= rows) return;
+  if (all) {
+    const int tok = R / p.G, h = hk * p.G + R - tok * p.G;
+    const float inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
+    uint16_t* y = (uint16_t*)p.Y + (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh + col;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) mg = fmaxf(mg, ml[64 * x + r]);
+    for (int x = 0; x < 4 * NB; x += 8)
+      *(u32x4*)(y + x) = u32x4{pack2_bf16(o[x] * inv, o[x + 1] * inv), pack2_bf16(o[x + 2] * inv, o[x + 3] * inv),
+                               pack2_bf16(o[x + 4] * inv, o[x + 5] * inv), pack2_bf16(o[x + 6] * inv, o[x + 7] * inv)};
+    if (p.lse && w == 0 && hl == 0) p.lse[(int64_t)h * p.T + s.q0 + tok] = sum == 0.f ? -INFINITY : (mg + log2f(sum)) * LN2;
+  } else {
+    const int64_t at = part_row(p, slot, hk, R);
+    float* y = (float*)p.ws + at * D + col;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) sum = fmaf(fast_exp2(ml[64 * x + r] - mg), ml[64 * x + 32 + r], sum);
-    const float mine = fast_exp2(m - mg);
-#pragma unroll
-    for (int e = 0; e < NB; ++e)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        part[((w * NB + e) * 4 + g) * 64 + lane] = make_float4(acc[e][4 * g] * mine, acc[e][4 * g + 1] * mine, acc[e][4 * g + 2] * mine, acc[e][4 * g + 3] * mine);
-    __syncthreads();
-    float o[4 * NB];
-#pragma unroll
-    for (int e = 0; e < NB; ++e) {
-      float4 x = part[((0 * NB + e) * 4 + w) * 64 + lane];
-#pragma unroll
-      for (int y = 1; y < 4; ++y) {
-        const float4 z = part[((y * NB + e) * 4 + w) * 64 + lane];
-        x.x += z.x; x.y += z.y; x.z += z.z; x.w += z.w;
-      }
-      o[e] = x.x; o[NB + e] = x.y; o[2 * NB + e] = x.z; o[3 * NB + e] = x.w;
-    }
-    const int R = r, col = NB * (8 * w + 4 * hl);
-    if (R >= rows) return;
-    if (f.parts == 1) {
-      const int tok = R / p.G, h = hk * p.G + R - tok * p.G;
-      const float inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
-      uint16_t* y = (uint16_t*)p.Y + (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh + col;
-#pragma unroll
-      for (int x = 0; x < 4 * NB; x += 8)
-        *(u32x4*)(y + x) = u32x4{pack2_bf16(o[x] * inv, o[x + 1] * inv), pack2_bf16(o[x + 2] * inv, o[x + 3] * inv),
-                                 pack2_bf16(o[x + 4] * inv, o[x + 5] * inv), pack2_bf16(o[x + 6] * inv, o[x + 7] * inv)};
-      if (p.lse && w == 0 && hl == 0) p.lse[(int64_t)h * p.T + s.q0 + tok] = sum == 0.f ? -INFINITY : (mg + log2f(sum)) * LN2;
-    } else {
-      const int64_t at = ((int64_t)slot * p.c.HK + hk) * p.max_rows + R;
-      float* y = (float*)p.ws + at * D + col;
-#pragma unroll
-      for (int x = 0; x < 4 * NB; x += 4) *(float4*)(y + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-      if (w == 0 && hl == 0) *(float2*)((float*)p.ws + p.ml_at + 2 * at) = make_float2(mg, sum);
-    }
+    for (int x = 0; x < 4 * NB; x += 4) *(float4*)(y + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+    if (w == 0 && hl == 0) *(float2*)((float*)p.ws + p.ml_at + 2 * at) = make_float2(mg, sum);
   }
 }
 
 template <int FMT, int D>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnP p) {
   __shared__ __attribute__((aligned(1024))) char smem[1024 + 4 * 32 * D * 4];
-  cache_attn_part<FMT, D>(p, smem);
+  const int piece = blockIdx.x / p.c.HK, hk = blockIdx.x - piece * p.c.HK;
+  const Cut cut(p);
+  for (int u = piece * cut.each, stop = min(u + cut.each, cut.total); u < stop;) {
+    const Run f = cut.find(u);
+    const int take = min(f.units - f.at, stop - u), begin = p.whole ? 0 : 128 * f.at, end = p.whole ? f.s.len : min(begin + 128 * take, f.s.len);
+    u += take;
+    cache_attn_run<FMT, D>(p, smem, f, hk, begin, end, take == f.units, part_slot(piece, cut.each, f.first));
+  }
 }
 
 // Rows of sequences in more than one part: W wavefronts per token and head.  D / 4 lanes take a part's columns, each of 64 W / (D / 4) groups of lanes
@@ -317,12 +316,14 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnP p) {
   const int unit = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave, t = unit / p.H, h = unit - t * p.H;
   if (t >= p.T) return;
   const Cut cut(p);
-  const Slot f = cut.owner(t);
-  if (f.b < 0 || f.parts < 2) return;
-  const int parts = f.parts, hk = h / p.G, R = (t - f.s.q0) * p.G + h - hk * p.G;
+  const Run f = cut.owner(t);
+  if (f.b < 0) return;
+  const int hk = h / p.G, R = (t - f.s.q0) * p.G + h - hk * p.G, group = Cut::many(p, f.s.n) ? R >> 7 : 0;
+  const int begin = f.first + group * f.units, piece = begin / cut.each, parts = (begin + f.units - 1) / cut.each - piece + 1;
+  if (parts < 2) return;
   const float* ws = (const float*)p.ws;
-  const int64_t first = ((int64_t)f.part * p.c.HK + hk) * p.max_rows + R, step = (int64_t)p.c.HK * p.max_rows;
-  const float2* ml = (const float2*)(ws + p.ml_at) + first;
+  const int64_t first = part_row(p, part_slot(piece, cut.each, begin), hk, R - 128 * group);
+  const int64_t second = part_row(p, part_slot(piece + 1, cut.each, begin), hk, R - 128 * group), step = part_row(p, 2, 0, 0);  // the first run of every piece to come
   float m = -1e30f, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
   for (int x0 = (W == 4 ? wave * GROUPS : 0) + lane / LANES; x0 < parts; x0 += 4 * STRIDE) {
     float4 o[4];
@@ -330,8 +331,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnP p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int x = min(x0 + i * STRIDE, parts - 1);
-      s[i] = ml[x * step];
-      o[i] = *(const float4*)(ws + (first + x * step) * D + 4 * c);
+      const int64_t at = x ? second + (x - 1) * step : first;
+      s[i] = *(const float2*)(ws + p.ml_at + 2 * at);
+      o[i] = *(const float4*)(ws + at * D + 4 * c);
     }
     float mn = m;
 #pragma unroll
@@ -397,44 +399,43 @@ void launch_join(const CacheAttnP& p, hipStream_t st) {
   else cache_join_kernel<D, 1><<<(int)((units + 3) / 4), 256, 0, st>>>(p);
 }
 
-// How the work is cut: from the descriptors alone.
+// How the work is cut (cache_cut.h): from the descriptors alone.
 void cut(CacheAttnP& p) {
   p.max_rows = p.max_new * p.G;
-  p.groups = (p.max_rows + 127) / 128;
-  const int64_t most = (int64_t)p.c.max_pages << p.c.shift;  // keys of a sequence
-  const int64_t want = 512 / ((int64_t)p.c.HK * p.groups);   // two work-groups to a compute unit
-  p.parts = (int)(want > 1 ? want : 1);
-  p.least = most <= 512 ? 512 : 256;  // a context that fits 512 keys is one part
-  p.slots = 2 * p.parts + p.c.n_seq;
-  p.ml_at = (int64_t)p.slots * p.c.HK * p.max_rows * p.c.D;
+  p.whole = ((int64_t)p.c.max_pages << p.c.shift) <= 512;
+  const int runs = p.c.n_seq * (p.max_rows <= 64 ? 1 : (p.max_rows + 127) / 128);
+  p.pieces = p.whole ? runs : p.c.HK < 512 ? 512 / p.c.HK : 1;  // two work-groups to a compute unit
+  p.least = p.whole ? 1 : 2;
+  p.part_rows = p.max_rows <= 64 ? p.max_rows : 128;
+  p.ml_at = part_row(p, 2 * p.pieces, 0, 0) * p.c.D;
 }
-bool one_part(const CacheAttnP& p) { return ((int64_t)p.c.max_pages << p.c.shift) <= p.least; }
 
 }  // namespace
 
 size_t cache_attn_bytes(const CacheAttnP& q) {
   CacheAttnP p = q;
   cut(p);
-  return one_part(p) ? 0 : (size_t)p.slots * p.c.HK * p.max_rows * (p.c.D + 2) * sizeof(float);
+  return p.whole ? 0 : (size_t)part_row(p, 2 * p.pieces, 0, 0) * (p.c.D + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_attn(const CacheAttnP& q, hipStream_t st) {
   CacheAttnP p = q;
   cut(p);
+  const int blocks = p.pieces * p.c.HK;
   auto by_size = [&](auto fmt) {
-    if (p.c.D == 64) launch<fmt(), 64>(p, p.slots * p.c.HK, st);
-    else launch<fmt(), 128>(p, p.slots * p.c.HK, st);
+    if (p.c.D == 64) launch<fmt(), 64>(p, blocks, st);
+    else launch<fmt(), 128>(p, blocks, st);
   };
   hipError_t e;
   if (p.max_rows > 32) {
-    e = launch_cache_attn_rows(p, (int)((((int64_t)p.slots * p.c.HK + 7) / 8) * 8 * p.groups), st);
+    e = launch_cache_attn_rows(p, blocks, st);
   } else {
     if (p.c.format == BF) by_size(std::integral_constant<int, BF>{});
     else if (p.c.format == F8) by_size(std::integral_constant<int, F8>{});
     else by_size(std::integral_constant<int, I8>{});
     e = hipGetLastError();
   }
-  if (e != hipSuccess || one_part(p)) return e;
+  if (e != hipSuccess || p.whole) return e;
   if (p.c.D == 64) launch_join<64>(p, st);
   else launch_join<128>(p, st);
   return hipGetLastError();

@@ -22,24 +22,19 @@ struct RowsLds {
   static constexpr int BYTES = SCALES + KG * 2 * 512;
 };
 
+// One run (or part of one) of a piece (as in cache_attn.hip), for 32 RB rows.
 template <int FMT, int D, int RB>
-__device__ __forceinline__ void cache_attn_rows(const CacheAttnP& p, char* smem) {
+__device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, const Run& f, int hk, int begin, int end, bool all, int slot) {
   using T = PTile<D>;
   using L = RowsLds<FMT, D, RB>;
   constexpr int KS = T::KS, DB = T::DB, KG = L::KG, KEYS = L::KEYS, NKB = L::NKB;
   constexpr int ROW_B = D * (FMT == BF ? 2 : 1), LPR = ROW_B / 16, NL = ROW_B / 64, RPL = 64 / LPR;  // lanes of a row; loads of 16 rows; rows of one
-  const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
+  int lane = threadIdx.x & 63;
+  asm("" : "+v"(lane));  // (what follows from it is formed anew for every run: kept over the loop, it spills)
+  const int r = lane & 31, hl = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rb = w % RB, kg = w / RB;
-  const int idx = blockIdx.x >> 3, unit = idx / p.groups * 8 + (int)(blockIdx.x & 7), rg = idx % p.groups;  // (as in cache_attn.hip)
-  const int slot = unit / p.c.HK, hk = unit - slot * p.c.HK;
-  if (slot >= p.slots) return;
-  const Cut cut(p);
-  const Slot f = cut.find(slot);
-  if (f.b < 0) return;
   const CacheSeq s = f.s;
-  const int rows = s.n * p.G, row0 = 32 * RB * rg;
-  if (row0 >= rows) return;
-  const int begin = f.part * cut.chunk, end = begin + min(cut.chunk, s.len - begin), shift = p.c.shift;
+  const int rows = s.n * p.G, row0 = 128 * f.group, shift = p.c.shift;
   const int steps = (end - begin + 63) >> 6;  // of 64 keys
 
   const int32_t* line = p.c.table + (int64_t)f.b * p.c.max_pages;
@@ -275,7 +270,6 @@ __device__ __forceinline__ void cache_attn_rows(const CacheAttnP& p, char* smem)
         for (int g = 0; g < 4; ++g) part[(4 * db + g) * 64] = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
     }
     __syncthreads();
-    if (kg == 1) return;
     const float m1 = ml[r], mg = fmaxf(m, m1), a0 = fast_exp2(m - mg), a1 = fast_exp2(m1 - mg);
     sum = fmaf(a1, ml[32 + r], a0 * l);
     m = mg;
@@ -290,7 +284,7 @@ __device__ __forceinline__ void cache_attn_rows(const CacheAttnP& p, char* smem)
         acc[db][4 * g + 3] = fmaf(a1, x.w, a0 * acc[db][4 * g + 3]);
       }
   }
-  if (f.parts == 1) {
+  if (kg == 0 && all) {
     const float inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
     uint16_t* y = (uint16_t*)p.Y + (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh;
 #pragma unroll
@@ -301,8 +295,8 @@ __device__ __forceinline__ void cache_attn_rows(const CacheAttnP& p, char* smem)
       store_row32(y + 32 * db, o, hl, live_row);
     }
     if (live_row && p.lse && hl == 0) p.lse[(int64_t)h * p.T + s.q0 + tok] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
-  } else if (live_row) {
-    const int64_t at = ((int64_t)slot * p.c.HK + hk) * p.max_rows + R;
+  } else if (kg == 0 && live_row) {
+    const int64_t at = part_row(p, slot, hk, R - row0);
     float* y = (float*)p.ws + at * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -311,19 +305,29 @@ __device__ __forceinline__ void cache_attn_rows(const CacheAttnP& p, char* smem)
         *(float4*)(y + 32 * db + 8 * g + 4 * hl) = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
     if (hl == 0) *(float2*)((float*)p.ws + p.ml_at + 2 * at) = make_float2(m, sum);
   }
+  __syncthreads();  // the next run's tiles come where this one's lay
 }
 
-template <int FMT, int D, int RB>
+template <int FMT, int D>
 __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnP p) {
-  __shared__ __attribute__((aligned(1024))) char smem[RowsLds<FMT, D, RB>::BYTES];
-  static_assert(RB == 4 || 1024 + RB * 32 * D * 4 <= RowsLds<FMT, D, RB>::BYTES, "the second pair's part fits");
-  cache_attn_rows<FMT, D, RB>(p, smem);
+  __shared__ __attribute__((aligned(1024))) char smem[RowsLds<FMT, D, 2>::BYTES];
+  static_assert(RowsLds<FMT, D, 2>::BYTES >= RowsLds<FMT, D, 4>::BYTES && RowsLds<FMT, D, 2>::BYTES >= 1024 + 2 * 32 * D * 4, "both forms and the second pair's part");
+  const int piece = blockIdx.x / p.c.HK, hk = blockIdx.x - piece * p.c.HK;
+  const Cut cut(p);
+  for (int u = piece * cut.each, stop = min(u + cut.each, cut.total); u < stop;) {
+    const Run f = cut.find(u);
+    const int sh = Cut::many(p, f.s.n) ? 6 : 7, take = min(f.units - f.at, stop - u);
+    const int begin = p.whole ? 0 : f.at << sh, end = p.whole ? f.s.len : min(begin + (take << sh), f.s.len);
+    u += take;
+    const int slot = part_slot(piece, cut.each, f.first);
+    if (sh == 6) cache_rows_run<FMT, D, 4>(p, smem, f, hk, begin, end, take == f.units, slot);
+    else cache_rows_run<FMT, D, 2>(p, smem, f, hk, begin, end, take == f.units, slot);
+  }
 }
 
 template <int FMT, int D>
 void launch(const CacheAttnP& p, int blocks, hipStream_t st) {
-  if (p.max_rows <= 64) cache_attn_rows_kernel<FMT, D, 2><<<blocks, 256, 0, st>>>(p);
-  else cache_attn_rows_kernel<FMT, D, 4><<<blocks, 256, 0, st>>>(p);
+  cache_attn_rows_kernel<FMT, D><<<blocks, 256, 0, st>>>(p);
 }
 
 }  // namespace

@@ -8,7 +8,7 @@ namespace {
 
 enum { BF = 0, F8 = 1, I8 = 2 };
 
-// What one sequence has: its new tokens' rows, the keys before them and in all, and the parts of `chunk` keys.
+// What one sequence has: its new tokens' rows, the keys before them and in all.
 struct CacheSeq {
   int q0, n, before, len;
 };
@@ -21,8 +21,6 @@ __device__ __forceinline__ CacheSeq cache_seq(const CacheAttnP& p, int b) {
   s.len = (int)min((int64_t)lens, (int64_t)p.c.max_pages << p.c.shift);  // keys that the table has a place for
   return s;
 }
-__device__ __forceinline__ int parts_of(const CacheSeq& s, int chunk) { return s.n > 0 ? (s.len > 0 ? (s.len - 1) / chunk + 1 : 1) : 0; }
-
 __device__ __forceinline__ int scan64(int x) {  // inclusive prefix sums over the wavefront
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
   x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
@@ -32,67 +30,75 @@ __device__ __forceinline__ int scan64(int x) {  // inclusive prefix sums over th
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
-__device__ __forceinline__ CacheSeq lane_seq(const CacheAttnP& p, int b) {
-  CacheSeq s = cache_seq(p, min(b, p.c.n_seq - 1));
-  if (b >= p.c.n_seq) s.n = s.len = 0;
-  return s;
-}
-// The parts of all sequences: a lane holds one, 64 at a time (up to 64 sequences: loaded once).
-struct Slot {
+
+// How the work is cut.  All keys of all sequences, for one key head, are one line of units, a unit being 128 keys (64 where a sequence has
+// more than 64 rows, which take twice as long; those go over the keys once for every 128 rows).  The line is dealt out in equal pieces of
+// `each` units to as many work-groups as the chip holds: they all end at the same time, however the lengths are spread.  A piece
+// may end in the middle of a sequence, whose parts are then joined by a second launch, and may hold several sequences one after the
+// other.  (Equal parts of every sequence, with as many work-groups, against this: ROUNDS)
+// Where no sequence has room for more than 512 keys, every run over the keys is a piece and nothing is joined.
+struct Run {  // over the keys of one sequence, for its rows of group `group`
   CacheSeq s;
-  int b, part, parts;
+  int b, group, first, units, at;  // `first`: its first unit on the line; `units` it has; `at`: the unit asked for, from there
 };
 struct Cut {
   const CacheAttnP& p;
-  CacheSeq mine;  // of the first 64
-  int chunk;      // keys of a part
-  __device__ __forceinline__ Cut(const CacheAttnP& q) : p(q) {
+  CacheSeq mine;     // of the first 64 sequences, a lane each
+  int total, each;
+  __device__ __forceinline__ Cut(const CacheAttnP& q) : p(q), total(0) {
     const int lane = threadIdx.x & 63;
-    mine = lane_seq(p, lane);
-    // Parts enough to fill the chip once (`p.parts` over all sequences), of p.least keys or more; where they would be long, half as long, down to
-    // 1024 keys: the sequences' last parts then leave less of the chip idle than the second round's starts cost.  One round | two |
-    // four, us: 64 sequences x 4000, 8 heads, e4m3, 137.6 | 125.6 | 124.5; 4 x 100000, int8, 227.0 | 173.0 | 190.8; 24 x 1500, 2 heads of 64 21.0 | 27.3 | 27.3.
-    int64_t total = 0;  // in units of 128 keys: the sum of 64 sequences of 2^31 keys fits an int
-    for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
-      const CacheSeq s = b0 ? lane_seq(p, b0 + lane) : mine;
-      total += __builtin_amdgcn_readlane(scan64(s.n > 0 ? (s.len >> 7) + 1 : 0), 63);
-    }
-    const int64_t once = (total + p.parts - 1) / p.parts * 128;
-    chunk = (int)max((int64_t)p.least, min(min(once, max((once + 255) / 256 * 128, (int64_t)1024)), (int64_t)0x7fffff80));
+    mine = at_lane(lane);
+    for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(scan64(line(b0 ? at_lane(b0 + lane) : mine)), 63);
+    each = max(p.least, (total + p.pieces - 1) / p.pieces);
   }
-  // the sequence of slot `slot`, and its part there; b = -1: fewer slots than that
-  __device__ __forceinline__ Slot find(int slot) const {
-    const int lane = threadIdx.x & 63;
-    Slot f;
+  __device__ __forceinline__ static bool many(const CacheAttnP& p, int n) { return n * p.G > 64; }
+  __device__ __forceinline__ int units(const CacheSeq& s) const {  // of one run
+    if (p.whole) return 1;
+    const int sh = many(p, s.n) ? 6 : 7;
+    return s.len > 0 ? ((s.len - 1) >> sh) + 1 : 1;
+  }
+  __device__ __forceinline__ int line(const CacheSeq& s) const { return s.n > 0 ? units(s) * (many(p, s.n) ? (s.n * p.G + 127) >> 7 : 1) : 0; }
+  __device__ __forceinline__ CacheSeq at_lane(int b) const {
+    CacheSeq s = cache_seq(p, min(b, p.c.n_seq - 1));
+    if (b >= p.c.n_seq) s.n = s.len = 0;
+    return s;
+  }
+  // the run that holds unit `u` < total of the line
+  __device__ __forceinline__ Run find(int u) const {
+    Run f;
     f.b = -1;
+    const int lane = threadIdx.x & 63;
+    int before = 0;
     for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
-      const CacheSeq s = b0 ? lane_seq(p, b0 + lane) : mine;
-      const int n = parts_of(s, chunk), upto = scan64(n), all = __builtin_amdgcn_readlane(upto, 63);
-      if (slot >= all) {
-        slot -= all;
-        continue;
+      const CacheSeq s = b0 ? at_lane(b0 + lane) : mine;
+      const int n = line(s), upto = scan64(n);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(u - before < upto);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        take(f, s, b0, l);
+        const int off = u - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+        f.group = off / f.units;
+        f.at = off - f.group * f.units;
+        f.first = u - f.at;
+        return f;
       }
-      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > slot));
-      take(f, s, b0, l, n);
-      f.part = slot - (__builtin_amdgcn_readlane(upto, l) - f.parts);
-      return f;
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
     return f;
   }
-  // the sequence of token t; `part`: the first of its slots
-  __device__ __forceinline__ Slot owner(int t) const {
-    const int lane = threadIdx.x & 63;
-    Slot f;
+  // the first run of token t's sequence; b = -1: a token of none, or behind the last that counts
+  __device__ __forceinline__ Run owner(int t) const {
+    Run f;
     f.b = -1;
+    const int lane = threadIdx.x & 63;
     int before = 0;
     for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
-      const CacheSeq s = b0 ? lane_seq(p, b0 + lane) : mine;
-      const int n = parts_of(s, chunk), upto = scan64(n);
+      const CacheSeq s = b0 ? at_lane(b0 + lane) : mine;
+      const int upto = scan64(line(s));
       const uint64_t hit = __builtin_amdgcn_ballot_w64(s.q0 <= t && t - s.q0 < s.n);
       if (hit) {
-        const int l = __builtin_ctzll(hit);
-        take(f, s, b0, l, n);
-        f.part = before + __builtin_amdgcn_readlane(upto, l) - f.parts;
+        take(f, s, b0, __builtin_ctzll(hit));
+        f.first = before + __builtin_amdgcn_readlane(upto, __builtin_ctzll(hit)) - line(f.s);
         return f;
       }
       before += __builtin_amdgcn_readlane(upto, 63);
@@ -101,15 +107,22 @@ struct Cut {
   }
 
  private:
-  __device__ __forceinline__ static void take(Slot& f, const CacheSeq& s, int b0, int l, int n) {
+  __device__ __forceinline__ void take(Run& f, const CacheSeq& s, int b0, int l) const {
     f.s.q0 = __builtin_amdgcn_readlane(s.q0, l);
     f.s.n = __builtin_amdgcn_readlane(s.n, l);
     f.s.before = __builtin_amdgcn_readlane(s.before, l);
     f.s.len = __builtin_amdgcn_readlane(s.len, l);
     f.b = b0 + l;
-    f.parts = __builtin_amdgcn_readlane(n, l);
+    f.units = units(f.s);
+    f.group = f.at = 0;
   }
 };
+// A piece's first run may have begun in an earlier piece, its last one may go on in the next: two slots for parts a piece.
+__device__ __forceinline__ int part_slot(int piece, int each, int first) { return 2 * piece + (first > piece * each ? 1 : 0); }
+// where a part's row lies in the workspace, in rows
+__host__ __device__ __forceinline__ int64_t part_row(const CacheAttnP& p, int slot, int hk, int row) {
+  return ((int64_t)slot * p.c.HK + hk) * p.part_rows + row;
+}
 
 // two 8-bit codes (bytes 2 HI and 2 HI + 1) as packed bf16, exactly
 template <int FMT, bool HI>

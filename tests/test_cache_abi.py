@@ -129,3 +129,56 @@ def test_rows_are_found_as_the_definition_says(tmp_path):
         page, row = (int(x) for x in line.split())
         assert (page, row) == ((-1, -1) if at is None else (at[0], (at[0] * 3 + 2) * 16 + at[1])), (b, pos)
     assert int(out[len(asked)]) == (30000000 * 96 + 95) * 1024 + 1023
+
+
+def _line(lens, new, G, whole=False):
+    """Units of every run of a key head's line, in order: (sequence, group of rows, units)."""
+    out = []
+    for b, (n_keys, n) in enumerate(zip(lens, new)):
+        many = n * G > 64
+        units = 1 if whole else max(1, -(-n_keys // (64 if many else 128)))
+        out += [(b, g, units) for g in range(-(-n * G // 128) if many else min(n, 1))]
+    return out
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_pieces_cover_the_line_and_parts_have_slots_of_their_own(seed):
+    """The arithmetic by which the kernels deal out keys and find each other's parts."""
+    rng = np.random.default_rng(seed)
+    for _ in range(60):
+        G, n_seq, pieces = int(rng.integers(1, 20)), int(rng.integers(1, 40)), int(rng.integers(1, 65))
+        lens, new = rng.integers(0, 4000, n_seq) * rng.integers(0, 2, n_seq), rng.integers(0, 40, n_seq)
+        runs = _line(lens, new, G)
+        total = sum(u for _, _, u in runs)
+        if not total:
+            continue
+        each = max(2, -(-total // pieces))
+        assert -(-total // each) <= pieces
+        written, first = {}, 0
+        starts = []
+        for b, g, units in runs:
+            starts.append(first)
+            first += units
+        for piece in range(pieces):  # as the attention's kernels go
+            u, stop = piece * each, min(piece * each + each, total)
+            while u < stop:
+                i = max(k for k, s in enumerate(starts) if s <= u)
+                at, units = u - starts[i], runs[i][2]
+                take = min(units - at, stop - u)
+                if take < units:
+                    slot = 2 * piece + (starts[i] > piece * each)
+                    assert slot < 2 * pieces and slot not in written
+                    written[slot] = (i, at, take)
+                u += take
+        for i, (b, g, units) in enumerate(runs):  # as the joining kernel does
+            begin = starts[i]
+            piece, parts = begin // each, (begin + units - 1) // each - begin // each + 1
+            if parts == 1:
+                assert all(w[0] != i for w in written.values())
+                continue
+            slots = [2 * piece + (begin > piece * each)] + [2 * (piece + x) + (begin > (piece + x) * each) for x in range(1, parts)]
+            assert slots[1:] == [2 * (piece + x) for x in range(1, parts)]
+            got = [written.pop(s) for s in slots]
+            assert [w[0] for w in got] == [i] * parts and sum(w[2] for w in got) == units
+            assert [w[1] for w in got] == list(np.cumsum([0] + [w[2] for w in got[:-1]]))
+        assert not written

@@ -88,6 +88,12 @@ ATTN = {
     "long": ([2900, 10, 777], [1, 1, 1], 8, 2, 128, 16),
     "empty_sequences": ([0, 40, 0], [0, 2, 0], 4, 2, 128, 16),
     "many_sequences": ([(37 * i) % 90 for i in range(150)], [i % 3 for i in range(150)], 4, 1, 64, 8),
+    "pieces": ([600, 5, 0, 1300, 90, 513], [3, 1, 2, 4, 0, 1], 8, 2, 128, 16),
+    "pieces_of_many": ([(61 * i) % 700 for i in range(100)], [i % 4 for i in range(100)], 4, 2, 64, 16),
+    "groups_of_rows": ([600, 5, 900, 1300, 0], [40, 3, 0, 64, 33], 8, 2, 128, 16),
+    "groups64": ([33, 1100, 640], [10, 64, 17], 24, 3, 64, 32),
+    "up_to_64_rows": ([800, 20, 450], [15, 16, 9], 12, 3, 128, 8),
+    "more_heads_than_work_groups": ([130, 3], [1, 1], 514, 514, 64, 1024),
 }
 
 
