@@ -11,12 +11,13 @@
 namespace ssa {
 namespace {
 
-template <int D, bool KEPT>
+template <int D, bool KEPT, int KG>
 __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   using T = PTile<D>;
   constexpr int KS = T::KS, DB = T::DB, U = T::LOADS / 4, STAGE_B = 4 * T::SUB_B;
   const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = KG == 2 ? wave & 3 : wave, kg = KG == 2 ? wave >> 2 : 0;
+  char* mine = smem + kg * 2 * STAGE_B;
   const PPlace at = p_place(p.h1 - p.h0);
   const PFound f = p_find<false, 7>(p, at.rank);
   if (f.t < 0) return;
@@ -51,10 +52,11 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
     }
   };
   uint32_t ka[KS], va[2][DB];
-  p_nat_addr<D>(ka, smem, r, hl);
-  p_tr_addr<D>(va, smem, lane);
+  p_nat_addr<D>(ka, mine, r, hl);
+  p_tr_addr<D>(va, mine, lane);
 
-  if (ntiles > 0) fetch_tile(smem, 0);
+  const int steps = (ntiles + KG - 1) / KG;  // a group's step i is key tile KG i + kg
+  if (steps > 0) fetch_tile(mine, kg);
   const int64_t qrow = (int64_t)(s.q0 + tok) * p.q_st + (int64_t)h * p.q_sh, yrow = (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh;
   bf16x8 qf[KS];
   u32x4 gf[KS];
@@ -79,7 +81,7 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
       }
     }
     delta = half_sum(part);
-    if (live && hl == 0) p.delta_out[di] = delta;
+    if (live && hl == 0 && kg == 0) p.delta_out[di] = delta;
   } else {
     delta = p.delta[di];
   }
@@ -127,12 +129,13 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] = mfma(w_frag2(kt_[hb][2 * db], kt_[hb][2 * db + 1]), df[hb], acc[db]);
   };
-  auto step = [&](auto sb, int kt) {
+  auto step = [&](auto sb, int i) {
     constexpr int SB = decltype(sb)::value;
-    W_VMCNT(0);  // this wavefront's part of tile kt has landed
+    const int kt = KG * i + kg;
+    W_VMCNT(0);  // this wavefront's part of the tile has landed
     __builtin_amdgcn_s_barrier();  // ... everybody's; and everybody is done with the other buffer
     asm volatile("" ::: "memory");
-    if (kt + 1 < ntiles) fetch_tile(smem + (STAGE_B - SB), kt + 1);
+    if (i + 1 < steps) fetch_tile(mine + (STAGE_B - SB), kt + KG);
     if (kt < wtiles) {
       const int k0 = kt * 64;
       const bool edge = k0 + 63 > first_pos;
@@ -140,12 +143,34 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
       half(std::integral_constant<int, SB + T::SUB_B>{}, std::integral_constant<int, SB + 3 * T::SUB_B>{}, k0 + 32, edge);
     }
   };
-  int kt = 0;
-  for (; kt + 1 < ntiles; kt += 2) {
-    step(std::integral_constant<int, 0>{}, kt);
-    step(std::integral_constant<int, STAGE_B>{}, kt + 1);
+  int i = 0;
+  for (; i + 1 < steps; i += 2) {
+    step(std::integral_constant<int, 0>{}, i);
+    step(std::integral_constant<int, STAGE_B>{}, i + 1);
   }
-  if (kt < ntiles) step(std::integral_constant<int, 0>{}, kt);
+  if (i < steps) step(std::integral_constant<int, 0>{}, i);
+  if (KG == 2) {  // the second group's sums, through LDS
+    float4* part = (float4*)smem + w * DB * 4 * 64 + lane;
+    __syncthreads();
+    if (kg == 1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) part[(4 * db + g) * 64] = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
+    }
+    __syncthreads();
+    if (kg == 1) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 x = part[(4 * db + g) * 64];
+        acc[db][4 * g] += x.x;
+        acc[db][4 * g + 1] += x.y;
+        acc[db][4 * g + 2] += x.z;
+        acc[db][4 * g + 3] += x.w;
+      }
+  }
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
     uint2 o[4];
@@ -156,17 +181,21 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   }
 }
 
-template <int D, bool KEPT>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void packed_dq_kernel(PackedP p) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 4 * PTile<D>::SUB_B];
-  packed_dq_tile<D, KEPT>(p, smem);
+template <int D, bool KEPT, int KG>
+__global__ __launch_bounds__(256 * KG, KG == 1 && D == 64 ? 3 : 2) void packed_dq_kernel(PackedP p) {
+  __shared__ __attribute__((aligned(1024))) char smem[KG * 2 * 4 * PTile<D>::SUB_B];
+  packed_dq_tile<D, KEPT, KG>(p, smem);
 }
 
 template <bool KEPT>
 hipError_t launch(const PackedP& p, hipStream_t st) {
   const int g = (int)p_blocks(p_most_tiles(p, false, 7), p.h1 - p.h0);
-  if (p.D <= 64) packed_dq_kernel<64, KEPT><<<g, 256, 0, st>>>(p);
-  else packed_dq_kernel<128, KEPT><<<g, 256, 0, st>>>(p);
+  auto by_groups = [&](auto d) {
+    if (p_two_groups(p)) packed_dq_kernel<d(), KEPT, 2><<<g, 512, 0, st>>>(p);
+    else packed_dq_kernel<d(), KEPT, 1><<<g, 256, 0, st>>>(p);
+  };
+  if (p.D <= 64) by_groups(std::integral_constant<int, 64>{});
+  else by_groups(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 

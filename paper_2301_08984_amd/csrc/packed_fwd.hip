@@ -2,7 +2,8 @@
 //
 // A work-group of four wavefronts owns a tile of 128 rows (packed_tile.h), a wavefront 32 of them, and walks the keys in blocks of 64
 // with the running maximum and sum of a softmax; K / V tiles travel from memory straight into two LDS buffers, one barrier a
-// block (as in fast_fwd128.hip, whose arithmetic this is).  P is rounded to bf16 for the product with V, which is what the matrix
+// block (as in fast_fwd128.hip, whose arithmetic this is).  KG = 2: two groups of four wavefronts take every other block of keys (p_two_groups) and are
+// joined at the end.  P is rounded to bf16 for the product with V, which is what the matrix
 // instructions take; scores, maxima, sums and O are fp32.
 #include "packed_tile.h"
 
@@ -11,12 +12,13 @@
 namespace ssa {
 namespace {
 
-template <int D, bool STAT>
+template <int D, bool STAT, int KG>
 __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
   using T = PTile<D>;
   constexpr int KS = T::KS, DB = T::DB, U = T::LOADS / 4, STAGE_B = 4 * T::SUB_B;
   const int lane = threadIdx.x & 63, r = lane & 31, hl = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = KG == 2 ? wave & 3 : wave, kg = KG == 2 ? wave >> 2 : 0;
+  char* mine = smem + kg * 2 * STAGE_B;
   const PPlace at = p_place(p.h1 - p.h0);
   const PFound f = p_find<false, 7>(p, at.rank);
   if (f.t < 0) return;
@@ -52,10 +54,11 @@ __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
     }
   };
   uint32_t ka[KS], va[2][DB];
-  p_nat_addr<D>(ka, smem, r, hl);
-  p_tr_addr<D>(va, smem, lane);
+  p_nat_addr<D>(ka, mine, r, hl);
+  p_tr_addr<D>(va, mine, lane);
 
-  if (ntiles > 0) fetch_tile(smem, 0);
+  const int steps = (ntiles + KG - 1) / KG;  // a group's step i is key tile KG i + kg
+  if (steps > 0) fetch_tile(mine, kg);
   bf16x8 qf[KS];
   {
     const uint16_t* q = (const uint16_t*)p.Q + (int64_t)(s.q0 + tok) * p.q_st + (int64_t)h * p.q_sh;
@@ -138,21 +141,50 @@ __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) oacc[db] = mfma(w_frag2(vu[t][2 * db], vu[t][2 * db + 1]), pf[2 + t], oacc[db]);
   };
-  auto step = [&](auto sb, int kt) {
+  auto step = [&](auto sb, int i) {
     constexpr int SB = decltype(sb)::value;
-    W_VMCNT(0);  // this wavefront's part of tile kt has landed
+    const int kt = KG * i + kg;
+    W_VMCNT(0);  // this wavefront's part of the tile has landed
     __builtin_amdgcn_s_barrier();  // ... everybody's; and everybody is done with the other buffer
     asm volatile("" ::: "memory");
-    if (kt + 1 < ntiles) fetch_tile(smem + (STAGE_B - SB), kt + 1);
+    if (i + 1 < steps) fetch_tile(mine + (STAGE_B - SB), kt + KG);
     if (kt < wtiles) tile(sb, kt * 64);
   };
-  int kt = 0;
-  for (; kt + 1 < ntiles; kt += 2) {
-    step(std::integral_constant<int, 0>{}, kt);
-    step(std::integral_constant<int, STAGE_B>{}, kt + 1);
+  int i = 0;
+  for (; i + 1 < steps; i += 2) {
+    step(std::integral_constant<int, 0>{}, i);
+    step(std::integral_constant<int, STAGE_B>{}, i + 1);
   }
-  if (kt < ntiles) step(std::integral_constant<int, 0>{}, kt);
+  if (i < steps) step(std::integral_constant<int, 0>{}, i);
 
+  if (KG == 2) {  // the second group's part, through LDS
+    float* ml = (float*)smem + 128 * w;
+    float4* part = (float4*)(smem + 2048) + w * DB * 4 * 64 + lane;
+    __syncthreads();
+    if (kg == 1) {
+      ml[lane] = l;
+      ml[64 + lane] = m;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) part[(4 * db + g) * 64] = make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]);
+    }
+    __syncthreads();
+    if (kg == 1) return;
+    const float m1 = ml[64 + lane], mg = fmaxf(m, m1), a0 = fast_exp2(m - mg), a1 = fast_exp2(m1 - mg);
+    l = fmaf(a1, ml[lane], a0 * l);
+    m = mg;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 x = part[(4 * db + g) * 64];
+        oacc[db][4 * g] = fmaf(a1, x.x, a0 * oacc[db][4 * g]);
+        oacc[db][4 * g + 1] = fmaf(a1, x.y, a0 * oacc[db][4 * g + 1]);
+        oacc[db][4 * g + 2] = fmaf(a1, x.z, a0 * oacc[db][4 * g + 2]);
+        oacc[db][4 * g + 3] = fmaf(a1, x.w, a0 * oacc[db][4 * g + 3]);
+      }
+  }
   const float sum = half_sum(l), inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
   const float lse = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
   const int64_t stat = (int64_t)(s.q0 + tok);
@@ -193,17 +225,22 @@ __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
   }
 }
 
-template <int D, bool STAT>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void packed_fwd_kernel(PackedP p) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 4 * PTile<D>::SUB_B];
-  packed_fwd_tile<D, STAT>(p, smem);
+template <int D, bool STAT, int KG>
+__global__ __launch_bounds__(256 * KG, D == 128 ? 2 : 4) void packed_fwd_kernel(PackedP p) {
+  __shared__ __attribute__((aligned(1024))) char smem[KG * 2 * 4 * PTile<D>::SUB_B];
+  static_assert(KG == 1 || sizeof(smem) >= 2048 + 4 * 32 * D * 4, "the second group's part fits");
+  packed_fwd_tile<D, STAT, KG>(p, smem);
 }
 
 template <bool STAT>
 hipError_t launch(const PackedP& p, hipStream_t st) {
   const int g = (int)p_blocks(p_most_tiles(p, false, 7), p.h1 - p.h0);
-  if (p.D <= 64) packed_fwd_kernel<64, STAT><<<g, 256, 0, st>>>(p);
-  else packed_fwd_kernel<128, STAT><<<g, 256, 0, st>>>(p);
+  auto by_groups = [&](auto d) {
+    if (p_two_groups(p)) packed_fwd_kernel<d(), STAT, 2><<<g, 512, 0, st>>>(p);
+    else packed_fwd_kernel<d(), STAT, 1><<<g, 256, 0, st>>>(p);
+  };
+  if (p.D <= 64) by_groups(std::integral_constant<int, 64>{});
+  else by_groups(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 

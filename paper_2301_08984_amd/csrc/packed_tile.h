@@ -221,6 +221,10 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
 // (row tiles: 128 * tiles <= Tq * G + 127 * n_seq; key tiles alike)
 inline int64_t p_most_tiles(const PackedP& p, bool keys, int sh) { return ((keys ? (int64_t)p.Tk : (int64_t)p.Tq * p.G) >> sh) + p.n_seq; }
 
+// Two groups of wavefronts share a tile of rows where there are too few tiles to keep the chip busy to the end with one: the longest tile then
+// takes half as long.  TWO_GROUPS
+inline bool p_two_groups(const PackedP& p) { return (((int64_t)p.Tq * p.G) >> 7) * p.share_heads < 640; }
+
 // 1 / ln 2 times the scale, never zero: a factor of 0 would make NaN of a masked score; any score times 2^-120 is 0
 // next to the exponents that matter.  Its sign goes into Q.
 __device__ __forceinline__ float p_factor(float scale) { return fmaxf(fabsf(scale) * LOG2E, 0x1p-120f); }
