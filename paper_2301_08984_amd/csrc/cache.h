@@ -61,19 +61,4 @@ size_t cache_attn_bytes(const CacheAttnP& p);
 hipError_t launch_cache_attn(const CacheAttnP& p, hipStream_t st);
 hipError_t launch_cache_attn_rows(const CacheAttnP& p, int blocks, hipStream_t st);  // more than 32 rows
 
-#ifdef __HIPCC__
-// The sequence whose packed tokens, by the n_seq + 1 offsets `cu`, hold row t (the same in all lanes of the wavefront);
-// -1: none.  64 offsets at a time: those that are at most t come first.
-__device__ inline int packed_owner(const int32_t* cu, int n_seq, int t) {
-  const int lane = threadIdx.x & 63;
-  int b = -1;
-  for (int b0 = 0; b0 < n_seq; b0 += 64) {
-    const int i = b0 + lane;
-    const uint64_t before = __builtin_amdgcn_ballot_w64(i < n_seq && cu[min(i, n_seq - 1)] <= t && t < cu[min(i, n_seq - 1) + 1]);
-    if (before) return b0 + 63 - __builtin_clzll(before);
-  }
-  return b;
-}
-#endif
-
 }  // namespace ssa

@@ -4,6 +4,7 @@
 // its K rows, one a head, and V rows behind them).  The largest magnitude goes round the row's lanes, every lane converts its
 // own eight values.  Bound by memory: 4 D bytes in and 2 D + 8 out for a token and head, or the reverse.
 #include "cache.h"
+#include "packed.h"
 #include "mfma_common.h"
 
 namespace ssa {

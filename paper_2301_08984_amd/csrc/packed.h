@@ -18,6 +18,8 @@ struct PackedP {
   float scale;
   int Tq, Tk, n_seq, H, HK, D, G;  // G = H / HK
   int h0, h1;                      // the chunk's key heads
+  int parts;                       // of the rows that a work-group of dK and dV takes; more than one: the parts' sums in dkdv_parts, [part][dV, dK][Tk][heads][D]
+  float* dkdv_parts;
   int share_heads;                 // key heads of the whole share: kernel-shape choices go by it, never by the chunk
 };
 
@@ -25,8 +27,21 @@ hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st);    // Yo, and ls
 hipError_t launch_packed_stat(const PackedP& p, hipStream_t st);   // lse_out and delta_out, recomputed
 hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);     // dQ; with Y given delta_out too, else from delta
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st);
+int packed_dkdv_parts(const PackedP& p);  // from the share, never from the chunk
 
 #ifdef __HIPCC__
+// The sequence whose packed tokens, by the n_seq + 1 offsets `cu`, hold row t (the same in all lanes of the wavefront);
+// -1: none.  64 offsets at a time: those that are at most t come first.
+__device__ inline int packed_owner(const int32_t* cu, int n_seq, int t) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < n_seq; b0 += 64) {
+    const int i = b0 + lane;
+    const uint64_t before = __builtin_amdgcn_ballot_w64(i < n_seq && cu[min(i, n_seq - 1)] <= t && t < cu[min(i, n_seq - 1) + 1]);
+    if (before) return b0 + 63 - __builtin_clzll(before);
+  }
+  return -1;
+}
+
 // One sequence: its first query row and queries, its first key row and keys.  Offsets are clamped, so that no row
 // outside the tensors is named whatever the array holds.
 struct PackedSeq { int q0, n, k0, m; };

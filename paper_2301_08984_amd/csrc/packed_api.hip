@@ -32,7 +32,7 @@ int validate(const ss_packed_desc* d) {
   const int64_t G = d->H / d->HK;
   if (G * d->q_stride_h + 33 * d->q_stride_t >= (int64_t)1 << 30 || G * d->y_stride_h + 33 * d->y_stride_t >= (int64_t)1 << 30) return SS_ERR_UNSUPPORTED;
   if (d->Tq > (1 << 30) || d->Tk > (1 << 30) || d->Tq * G >= (1 << 30)) return SS_ERR_UNSUPPORTED;
-  if ((((d->Tq * G > d->Tk ? d->Tq * G : d->Tk) >> 7) + d->n_seq + 8) * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
+  if ((((d->Tq * G > 4ll * d->Tk ? d->Tq * G : 4ll * d->Tk) >> 7) + d->n_seq + 8) * 4 * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   if (d->lo < 0 || d->lo >= d->hi || d->hi > d->HK) return SS_ERR_BAD_RANGE;
   if (d->k < 1 || d->k > d->hi - d->lo) return SS_ERR_BAD_K;
   return SS_OK;
@@ -44,14 +44,30 @@ void chunk(const ss_packed_desc* d, int k, int c, int* a, int* b) {
   *b = d->lo + (int)(((c + 1) * n) / k);
 }
 
-// The scratch of one chunk: LSE (unless the caller kept it) and Delta of its query heads.
+PackedP params(const ss_packed_desc* d) {
+  PackedP p{};
+  p.q_st = d->q_stride_t; p.q_sh = d->q_stride_h;
+  p.k_st = d->k_stride_t; p.k_sh = d->k_stride_h;
+  p.y_st = d->y_stride_t; p.y_sh = d->y_stride_h;
+  p.scale = d->scale;
+  p.Tq = d->Tq; p.Tk = d->Tk; p.n_seq = d->n_seq;
+  p.H = d->H; p.HK = d->HK; p.D = d->D; p.G = d->H / d->HK;
+  p.h0 = d->lo; p.h1 = d->hi;
+  p.share_heads = d->hi - d->lo;
+  return p;
+}
+
+// The scratch of one chunk: LSE (unless the caller kept it) and Delta of its query heads, and the parts of dK and dV.
 struct Ws {
-  size_t lse, delta, total;
+  size_t lse, parts, total;
 };
 Ws layout(const ss_packed_desc* d, int k, bool kept) {
   const int64_t n = d->hi - d->lo, most = (n + k - 1) / k;  // key heads of the largest chunk
   const size_t stat = align256((size_t)(most * (d->H / d->HK)) * d->Tq * 4);
-  return Ws{stat, 0, kept ? stat : 2 * stat};
+  const int parts = ssa::packed_dkdv_parts(params(d));
+  Ws w{stat, kept ? stat : 2 * stat, 0};
+  w.total = w.parts + (parts > 1 ? align256((size_t)parts * 2 * d->Tk * most * d->D * 4) : 0);
+  return w;
 }
 // The fewest chunks, at most d->k, whose scratch fits `bytes`: 1, 2, 4, .. (every number gives the same results).
 int fewest_chunks(const ss_packed_desc* d, bool kept, size_t bytes) {
@@ -71,19 +87,6 @@ int hip_fail(hipError_t e, const char* what) {
   } while (0)
 
 bool misaligned(const void* p) { return (uintptr_t)p & 15; }
-
-PackedP params(const ss_packed_desc* d) {
-  PackedP p{};
-  p.q_st = d->q_stride_t; p.q_sh = d->q_stride_h;
-  p.k_st = d->k_stride_t; p.k_sh = d->k_stride_h;
-  p.y_st = d->y_stride_t; p.y_sh = d->y_stride_h;
-  p.scale = d->scale;
-  p.Tq = d->Tq; p.Tk = d->Tk; p.n_seq = d->n_seq;
-  p.H = d->H; p.HK = d->HK; p.D = d->D; p.G = d->H / d->HK;
-  p.h0 = d->lo; p.h1 = d->hi;
-  p.share_heads = d->hi - d->lo;
-  return p;
-}
 
 }  // namespace
 
@@ -154,10 +157,12 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
   PackedP p = params(d);
   p.Q = Q; p.K = K; p.V = V; p.Y = Y; p.dY = dY; p.dQ = dQ; p.dK = dK; p.dV = dV;
   p.cu_q = cu_q; p.cu_k = cu_k ? cu_k : cu_q;
+  p.parts = ssa::packed_dkdv_parts(p);
+  p.dkdv_parts = (float*)(ws + w.parts);
   for (int c = 0; c < k; ++c) {
     chunk(d, k, c, &p.h0, &p.h1);
     p.delta_h0 = p.h0 * p.G;
-    p.delta_out = (float*)(ws + w.delta);
+    p.delta_out = (float*)ws;
     p.delta = p.delta_out;
     if (kept) {
       p.lse = lse;  // (Delta: by the kernel of dQ)

@@ -53,7 +53,7 @@ __device__ __forceinline__ void quads_issue(u32x4 (&f)[4], uint32_t at) {
 }
 
 template <int D, int RG, bool DK>  // DK: the second wavefront of a pair
-__device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, const PackedSeq& s, int tile, int hk) {
+__device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, const PackedSeq& s, int tile, int hk, int part) {
   using T = PTile<D>;
   using L = KvLds<D, RG>;
   constexpr int KS = T::KS, DB = T::DB, KB = 4 / RG, TK = 32 * KB;
@@ -65,7 +65,9 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
   const int k0 = tile * TK + 32 * kblock, key = k0 + r;
   const float c1 = p_factor(p.scale);
   const int tok0 = max(tile * TK - more, 0);  // the first token that sees the tile's first key
-  const int first = tok0 < s.n ? tok0 * G / 32 : 0, steps = tok0 < s.n ? (rows + 31) / 32 - first : 0;
+  const int from = tok0 < s.n ? tok0 * G / 32 : 0, all = tok0 < s.n ? (rows + 31) / 32 - from : 0;
+  const int first = from + (int)((int64_t)all * part / p.parts), steps = from + (int)((int64_t)all * (part + 1) / p.parts) - first;  // this part's
+  const int stop = min(rows, 32 * (first + steps));  // this part's rows end here
   const int n = (steps + RG - 1) / RG, row0 = 32 * (first + group);  // of a group; a group's step t begins at row row0 + 32 RG t
   const int dtok = 32 * RG / G, dg = 32 * RG % G;
   char* ring = smem + group * L::RING_B;
@@ -88,7 +90,7 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
   // the group's step t into its slot, in order (past the last step and the last row: zeros arrive); the statistics travel through registers of
   // one wavefront of each kind, asked for before the rows so that waiting for them leaves those under way
   auto fetch = [&](char* slot, int t) {
-    const int left = rows - (row0 + 32 * RG * t);
+    const int left = stop - (row0 + 32 * RG * t);
     if (kblock == 0) {
       const bool there = r < left;
       const int64_t at = (int64_t)(hk * G + own.g - (DK ? p.delta_h0 : p.lse_h0)) * p.Tq + s.q0 + own.tok;
@@ -275,6 +277,19 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
     }
   }
   if (group > 0) return;
+  if (p.parts > 1) {
+    float* out = p.dkdv_parts + (((int64_t)(2 * part + (DK ? 1 : 0)) * p.Tk + s.k0 + min(key, s.m - 1)) * (p.h1 - p.h0) + hk - p.h0) * p.D;
+    const float scale = DK ? p.scale : 1.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int col = 32 * db + 8 * g + 4 * hl;
+        if (key < s.m && col < p.D)
+          *(float4*)(out + col) = make_float4(acc[db][4 * g] * scale, acc[db][4 * g + 1] * scale, acc[db][4 * g + 2] * scale, acc[db][4 * g + 3] * scale);
+      }
+    return;
+  }
   uint16_t* out = (uint16_t*)(DK ? p.dK : p.dV) + (int64_t)(s.k0 + min(key, s.m - 1)) * p.k_st + (int64_t)hk * p.k_sh;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -290,26 +305,61 @@ template <int D, int RG>
 __global__ __launch_bounds__(512, 2) void packed_dkdv_kernel(PackedP p) {
   __shared__ __attribute__((aligned(1024))) char smem[KvLds<D, RG>::BYTES];
   static_assert(sizeof(smem) <= 160 * 1024 && (RG == 1 || 8 * 32 * D * 4 <= KvLds<D, RG>::STAT), "the groups' sums fit, too");
-  const PPlace at = p_place(p.h1 - p.h0);
+  const PPlace at = p_place((p.h1 - p.h0) * p.parts);
   const PFound f = p_find<true, RG == 1 ? 7 : RG == 2 ? 6 : 5>(p, at.rank);
   if (f.t < 0) return;
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8)) packed_kv_wave<D, RG, true>(p, smem, f.s, f.t, p.h0 + at.head);
-  else packed_kv_wave<D, RG, false>(p, smem, f.s, f.t, p.h0 + at.head);
+  const int head = at.head / p.parts, part = at.head - head * p.parts;
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8)) packed_kv_wave<D, RG, true>(p, smem, f.s, f.t, p.h0 + head, part);
+  else packed_kv_wave<D, RG, false>(p, smem, f.s, f.t, p.h0 + head, part);
+}
+
+// The parts of dK and dV, added up in order: a wavefront per key row (of a sequence: other rows stay as they were).
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedP p) {
+  const int lane = threadIdx.x & 63, t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (t >= p.Tk || packed_owner(p.cu_k, p.n_seq, t) < 0) return;
+  const int heads = p.h1 - p.h0, row = heads * p.D;  // values
+  for (int i = 4 * lane; i < 2 * row; i += 256) {
+    const bool dk = i >= row;
+    const int at = dk ? i - row : i, h = at / p.D;
+    const float* from = p.dkdv_parts + ((int64_t)(dk ? 1 : 0) * p.Tk + t) * row + at;
+    float4 x = *(const float4*)from;
+    for (int part = 1; part < p.parts; ++part) {
+      const float4 y = *(const float4*)(from + (int64_t)2 * part * p.Tk * row);
+      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    }
+    *(uint2*)((uint16_t*)(dk ? p.dK : p.dV) + (int64_t)t * p.k_st + (int64_t)(p.h0 + h) * p.k_sh + (at - h * p.D)) = pack4_bf16(x.x, x.y, x.z, x.w, 1.f);
+  }
 }
 
 template <int D, int RG>
 hipError_t launch(const PackedP& p, hipStream_t st) {
-  packed_dkdv_kernel<D, RG><<<(int)p_blocks(p_most_tiles(p, true, RG == 1 ? 7 : RG == 2 ? 6 : 5), p.h1 - p.h0), 512, 0, st>>>(p);
+  packed_dkdv_kernel<D, RG><<<(int)p_blocks(p_most_tiles(p, true, RG == 1 ? 7 : RG == 2 ? 6 : 5), (p.h1 - p.h0) * p.parts), 512, 0, st>>>(p);
+  if (p.parts > 1) packed_join_kernel<<<(p.Tk + 3) / 4, 256, 0, st>>>(p);
   return hipGetLastError();
+}
+
+// row groups of a work-group
+int row_groups(const PackedP& p) {
+  const int64_t tiles = (int64_t)(p.Tk >> 7) * p.share_heads;
+  if (p.D > 64) return tiles < 512 ? 2 : 1;
+  return tiles < 256 ? 4 : tiles < 512 ? 2 : 1;
 }
 
 }  // namespace
 
+// Where a launch has few work-groups and sequences are long, the longest of them, which walk most rows, keep the chip waiting: their rows
+// are then cut into two parts.  One part | two | four, us: 6007 tokens x 16 heads of 64 in groups of eight, 11 documents, 214 | 138 | 158.
+int packed_dkdv_parts(const PackedP& p) {
+  const int rg = row_groups(p);
+  const int64_t groups = ((int64_t)p.Tk * rg >> 7) * p.share_heads, rows = (int64_t)p.Tq * p.G / p.n_seq;
+  if (groups >= 768 || rows < 2048) return 1;
+  return (int64_t)4 * p.Tk * p.share_heads * p.D * 4 > (24 << 20) ? 1 : 2;  // (what the parts' sums may add to the workspace)
+}
+
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st) {
-  const int64_t tiles = (int64_t)(p.Tk >> 7) * p.share_heads;
-  if (p.D > 64) return tiles < 512 ? launch<128, 2>(p, st) : launch<128, 1>(p, st);
-  if (tiles < 256) return launch<64, 4>(p, st);
-  return tiles < 512 ? launch<64, 2>(p, st) : launch<64, 1>(p, st);
+  const int rg = row_groups(p);
+  if (p.D > 64) return rg == 2 ? launch<128, 2>(p, st) : launch<128, 1>(p, st);
+  return rg == 4 ? launch<64, 4>(p, st) : rg == 2 ? launch<64, 2>(p, st) : launch<64, 1>(p, st);
 }
 
 }  // namespace ssa

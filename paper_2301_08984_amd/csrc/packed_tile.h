@@ -113,6 +113,15 @@ __device__ __forceinline__ int p_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
+__device__ __forceinline__ int p_max(int x) {  // of the wavefront's non-negative numbers
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ int p_total(int x) { return __builtin_amdgcn_readlane(p_scan(x), 63); }
 
 // A launch's work-groups: 8 XCDs with an L2 each are dealt them in turn.  Every XCD gets HK / 8 whole key heads, whose K and V
@@ -187,9 +196,7 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
     const PackedSeq s = of_lane(0);
     if (rank >= p_total(p_tiles<KEYS, SH>(s, G))) return f;
     int lo = 0, hi = p_steps<KEYS, SH>(s, G);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) hi = max(hi, __shfl_xor(hi, o));
-    hi = __builtin_amdgcn_readfirstlane(hi) + 1;
+    hi = p_max(hi) + 1;
     while (hi - lo > 1) {  // more than `rank` tiles have `lo` steps or more, not as many have `hi`
       const int mid = (lo + hi) >> 1;
       if (p_total(p_at_least<KEYS, SH>(s, G, mid)) > rank) lo = mid;

@@ -28,6 +28,9 @@ CASES = {
     "fewer_keys": ([40, 100, 70, 3], [7, 37, 0, 3], 4, 2, 128),
     "no_queries": ([0, 20, 0], [30, 20, 129], 2, 1, 64),
     "many_sequences": ([3, 40, 0, 17] * 40, None, 4, 2, 64),
+    "parts": ([900, 40], None, 12, 2, 128),
+    "parts64": ([1100], [1300], 8, 1, 64),
+    "parts_odd_head": ([700, 0, 300], None, 16, 2, 72),
     "many_tiles": ([64] * 66 + [130], None, 32, 16, 128),
     "many_tiles64": ([70] * 60 + [131], None, 32, 16, 64),
     "some_tiles": ([64] * 66 + [130], None, 16, 8, 128),
