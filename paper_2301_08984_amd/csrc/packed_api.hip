@@ -28,9 +28,9 @@ int validate(const ss_packed_desc* d) {
   const int64_t lim = (int64_t)1 << 24;
   if (d->q_stride_t >= lim || d->q_stride_h >= lim || d->k_stride_t >= lim || d->k_stride_h >= lim || d->y_stride_t >= lim || d->y_stride_h >= lim)
     return SS_ERR_UNSUPPORTED;
-  // ... and a step's 32 rows of (token, head) pairs too; rows and work-groups are counted in 31 bits
+  // ... and a step's 32 rows of (token, head) pairs too, whose buffer descriptors end at 0x7e000000 bytes; rows and work-groups are counted in 31 bits
   const int64_t G = d->H / d->HK;
-  if (G * d->q_stride_h + 33 * d->q_stride_t >= (int64_t)1 << 30 || G * d->y_stride_h + 33 * d->y_stride_t >= (int64_t)1 << 30) return SS_ERR_UNSUPPORTED;
+  if (G * d->q_stride_h + 33 * d->q_stride_t >= 1000000000ll || G * d->y_stride_h + 33 * d->y_stride_t >= 1000000000ll) return SS_ERR_UNSUPPORTED;
   if (d->Tq > (1 << 30) || d->Tk > (1 << 30) || d->Tq * G >= (1 << 30)) return SS_ERR_UNSUPPORTED;
   if ((((d->Tq * G > 4ll * d->Tk ? d->Tq * G : 4ll * d->Tk) >> 7) + d->n_seq + 8) * 4 * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   if (d->lo < 0 || d->lo >= d->hi || d->hi > d->HK) return SS_ERR_BAD_RANGE;
@@ -139,7 +139,8 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
   hipStream_t st = (hipStream_t)hip_stream;
   // A chunk of few heads leaves most of the chip idle, and what keeps chunks apart is only that they reuse one chunk's scratch:
   // run the fewest whose scratch fits the caller's workspace, or else half of the library's buffer if nobody is using it.
-  // SPEEDUP
+  // One chunk | two | four | eight as asked, then the same merged, us: 9 documents, 4496 tokens, 32 heads of 128 in groups of four,
+  // recomputed, 261 | 408 | 755 | 1484, 261 | 269 | 250 | 244; one document of 8192, one | eight, 2447 | 10669, 2438 | 2415.
   const bool kept = lse != nullptr;
   char* ws = (char*)workspace;
   int k = fewest_chunks(d, kept, workspace_bytes);

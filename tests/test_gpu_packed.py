@@ -31,6 +31,11 @@ CASES = {
     "parts": ([900, 40], None, 12, 2, 128),
     "parts64": ([1100], [1300], 8, 1, 64),
     "parts_odd_head": ([700, 0, 300], None, 16, 2, 72),
+    "short_rows": ([64] * 95 + [130, 1, 0, 300], None, 32, 16, 128),
+    "short_and_long": ([100] * 50 + [400, 0, 700, 33, 129], None, 32, 4, 128),
+    "short64": ([107] * 60 + [200, 3], None, 32, 8, 64),
+    "short_five_key_heads": ([90] * 63 + [250], None, 35, 5, 96),
+    "short_more_keys": ([40, 90, 10] * 50, [100, 90, 7] * 50, 32, 8, 128),
     "many_tiles": ([64] * 66 + [130], None, 32, 16, 128),
     "many_tiles64": ([70] * 60 + [131], None, 32, 16, 64),
     "some_tiles": ([64] * 66 + [130], None, 16, 8, 128),

@@ -97,3 +97,15 @@ def test_chunks_and_workspace():
     # the scratch of the backward is one chunk's
     sizes = [pb.ss_packed_workspace_bytes(pb.make_desc(8192, 20, 32, 8, 128, 0, 8, k))[1] for k in (1, 2, 4, 8)]
     assert all(a >= 1.9 * b for a, b in zip(sizes, sizes[1:])), sizes
+
+
+def test_heads_and_tokens_of_a_step_that_lie_too_far_apart():
+    # 28 heads and 33 tokens, each 2^24 - 8 elements apart: 1.02e9 elements, further than a lane's offset reaches
+    far = (1 << 24) - 8
+    d = pb.make_desc(100, 3, 28, 1, 128, 0, 1, 1)
+    d.q_stride_t, d.q_stride_h = far, far
+    with pytest.raises(ss.SSAttnError) as e:
+        pb.ss_packed_workspace_bytes(d)
+    assert e.value.code == ss.SS_ERR_UNSUPPORTED
+    d.H = 26
+    assert pb.ss_packed_workspace_bytes(d)[1] > 0
