@@ -6,7 +6,7 @@
 // 64 keys; with up to 64 rows two of them share tiles of 32 keys, and the two pairs, with every other tile, are joined through LDS at the
 // end.  The codes of the next tile travel into registers while a tile is at work, and are converted into the other buffer after it.
 // With these rows in the registers of one wavefront instead (64 of them, every wavefront converting its own keys): 343 drafts
-// of 16 trees over 48000 keys, 8 key heads, e4m3: 84 us; 107 rows of 64 columns over 36000 keys, int8: 17.
+// of 16 trees over 48000 keys, 8 key heads, e4m3: 84 us against 64; 24 sequences of 8 tokens, groups of eight heads of 64, over 36000 keys, int8: 17 against 14.
 #include "cache_cut.h"
 #include "packed_tile.h"
 
@@ -61,13 +61,7 @@ __device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, 
   uint32_t ka[KS], va[2][DB];
   p_nat_addr<D>(ka, mine, r, hl);
   p_tr_addr<D>(va, mine, lane);
-  // this wavefront's 16 rows of a tile: where lanes put them
-  uint32_t put[NL], live_next = 0, live_hi_next = 0;
-#pragma unroll
-  for (int u = 0; u < NL; ++u) {
-    const int row = 16 * rb + RPL * u + lane / LPR, c = (lane % LPR) * (FMT == BF ? 1 : 2);
-    put[u] = (uint32_t)(row & 31) * (2 * D) + (uint32_t)(row >> 5) * T::SUB_B + (uint32_t)((c ^ p_sw<D>(row & 31)) << 4);
-  }
+  uint32_t live_next = 0, live_hi_next = 0;
   u32x4 kx[NL], vx[NL];
   float scale = 0.f;
   uint32_t here = 0;  // of these 16 keys, those that are there (looked at when the loads have arrived)
@@ -108,6 +102,14 @@ __device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, 
   // ... and puts it into buffer `to`
   auto stage = [&](int to) {
     char* tile = mine + to * L::TILE_B;
+    int lane = threadIdx.x & 63;
+    if (FMT == BF) asm("" : "+v"(lane));  // (as above)
+    uint32_t put[NL];  // this wavefront's 16 rows of a tile: where lanes put them
+#pragma unroll
+    for (int u = 0; u < NL; ++u) {
+      const int row = 16 * rb + RPL * u + lane / LPR, c = (lane % LPR) * (FMT == BF ? 1 : 2);
+      put[u] = (uint32_t)(row & 31) * (2 * D) + (uint32_t)(row >> 5) * T::SUB_B + (uint32_t)((c ^ p_sw<D>(row & 31)) << 4);
+    }
     if (here != 0xffffu) {  // what lies in other slots may be anything
 #pragma unroll
       for (int u = 0; u < NL; ++u) {

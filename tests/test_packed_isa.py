@@ -1,4 +1,4 @@
-"""The kernels of packed attention read LDS from hand-written assembly: nothing touches a register between a read and its
+"""The kernels of packed attention, and of many rows over the cache, read LDS from hand-written assembly: nothing touches a register between a read and its
 wait, no accumulation register is in use, and nothing is spilled (test_wave_isa.py, whose checks these are)."""
 import os
 import subprocess
@@ -9,7 +9,7 @@ from paper_2301_08984_amd import build as B
 from test_wave_isa import pending_read_violations
 
 
-@pytest.mark.parametrize("src", ["packed_fwd.hip", "packed_dq.hip", "packed_dkdv.hip"])
+@pytest.mark.parametrize("src", ["packed_fwd.hip", "packed_dq.hip", "packed_dkdv.hip", "cache_attn_rows.hip"])
 def test_generated_code(src, tmp_path):
     out = str(tmp_path / "k.s")
     r = subprocess.run(["hipcc", *B.FLAGS, *B.EXTRA_FLAGS[src], "--cuda-device-only", "-S", os.path.join(B.CSRC, src), "-o", out],
