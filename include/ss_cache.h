@@ -83,8 +83,9 @@ int ss_cache_attn_workspace_bytes(const ss_cache_desc* desc, const ss_cache_attn
  *             tokens (one new token: plain decoding).
  *   Y    out: the rows of the sequences; a row that sees nothing is 0.   lse out: float [H, T], or NULL; -inf for such a row.
  *             Rows of no sequence, and a sequence's rows from max_new on, are left as they were.
- * The keys are cut into parts of about equal length over all sequences, which run side by side and are joined by a second
- * launch where a sequence has more than one, in a fixed order: the same call gives the same bits.
+ * The keys of all sequences together are cut into pieces of equal length, which run side by side; where a sequence lies in
+ * more than one, its parts are joined by a second launch, in a fixed order: the same call gives the same bits.  (Where the cuts
+ * fall depends on the other sequences of the call, and with it the last bits of a row.)
  *   workspace : 256-byte aligned, need not start at zero.
  * What lies in slots behind a sequence's end has no influence.  In SS_CACHE_BF16 the V of a new token that another new
  * token does not see has to be finite (it is multiplied by a probability of zero); in 8 bits it may be anything. */

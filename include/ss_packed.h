@@ -51,7 +51,8 @@ typedef struct {
   uint32_t flags;    /* 0                                                            */
 } ss_packed_desc;
 
-/* Workspace bytes (host outputs, either may be NULL).  Forward: 0.  Backward: one chunk's statistics (LSE and Delta). */
+/* Workspace bytes (host outputs, either may be NULL).  Forward: 0.  Backward: one chunk's statistics (LSE and Delta)
+ * and, where the work of dK and dV is cut into parts because it is little, one chunk's share of up to 24 MiB for the parts' sums. */
 int ss_packed_workspace_bytes(const ss_packed_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes);
 
 /* The key heads of chunk c (0 <= c < k): lo + floor(c*n/k) .. lo + floor((c+1)*n/k), n = hi-lo. */

@@ -35,7 +35,8 @@ __device__ __forceinline__ int scan64(int x) {  // inclusive prefix sums over th
 // more than 64 rows, which take twice as long; those go over the keys once for every 128 rows).  The line is dealt out in equal pieces of
 // `each` units to as many work-groups as the chip holds: they all end at the same time, however the lengths are spread.  A piece
 // may end in the middle of a sequence, whose parts are then joined by a second launch, and may hold several sequences one after the
-// other.  (Equal parts of every sequence, with as many work-groups, against this: ROUNDS)
+// other.  (Equal parts of every sequence, with as many work-groups, against this, us: 64 conversations, 256000 keys, 8 key
+// heads, e4m3, 125 | 112; 4 of 400012 keys together, int8, 172 | 162; 16 trees over 48016 keys 95 | 75.)
 // Where no sequence has room for more than 512 keys, every run over the keys is a piece and nothing is joined.
 struct Run {  // over the keys of one sequence, for its rows of group `group`
   CacheSeq s;

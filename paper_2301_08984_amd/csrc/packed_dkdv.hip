@@ -10,6 +10,10 @@
 // KB x RG: the pairs take KB blocks of 32 keys, and RG groups of them every RG-th step each; the groups' sums are added up
 // through LDS at the end, in order.  With few keys and key heads a work-group of 128 keys walks far more rows than there are
 // work-groups to fill the chip; the rows are then read by more work-groups.
+//
+// Measured: one document of 16384 tokens, 12 heads of 128, 1886 us, 870 TFLOP/s, bound by LDS and vector instructions between the products;
+// 23 documents, 8192 tokens, 12 heads in groups of three: 60 us; 11 documents, 6007 tokens, 16 heads of 64 in groups of eight: 134 us,
+// bound by the rows that a work-group walks one after the other.
 #include "packed_tile.h"
 
 #include <type_traits>
@@ -338,7 +342,9 @@ hipError_t launch(const PackedP& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-// row groups of a work-group
+// Row groups of a work-group: more where there are few tiles of keys.  One | two | four, us: 8192 tokens, 23 documents, 12 heads in groups of three of 128,
+// 86 | 60; one document of 16384, 12 heads, 1886 | 2147; 6007 tokens, 11 documents, 16 heads of 64 in groups of eight, 293 | 190 | 134.
+// (Heads of 128 in four groups do not fit LDS.)
 int row_groups(const PackedP& p) {
   const int64_t tiles = (int64_t)(p.Tk >> 7) * p.share_heads;
   if (p.D > 64) return tiles < 512 ? 2 : 1;

@@ -229,7 +229,9 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
 inline int64_t p_most_tiles(const PackedP& p, bool keys, int sh) { return ((keys ? (int64_t)p.Tk : (int64_t)p.Tq * p.G) >> sh) + p.n_seq; }
 
 // Two groups of wavefronts share a tile of rows where there are too few tiles to keep the chip busy to the end with one: the longest tile then
-// takes half as long.  TWO_GROUPS
+// takes half as long.  One group | two, us, tiles x heads: 6 turns of 2000 tokens over a cache, 32 heads, 165 | 131; 11 documents, 16 heads of 64
+// in groups of eight, backward, 318 | 306; but 23 documents of 8192 tokens, 12 heads in groups of three, 131 | 167, and 19 prompts
+// of 9001 tokens, 32 heads, 91 | 124 (two groups cost a join and half of the work-groups on a CU).
 inline bool p_two_groups(const PackedP& p) { return (((int64_t)p.Tq * p.G) >> 7) * p.share_heads < 640; }
 
 // 1 / ln 2 times the scale, never zero: a factor of 0 would make NaN of a masked score; any score times 2^-120 is 0
