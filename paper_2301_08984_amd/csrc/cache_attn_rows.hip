@@ -103,7 +103,7 @@ __device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, 
   auto stage = [&](int to) {
     char* tile = mine + to * L::TILE_B;
     int lane = threadIdx.x & 63;
-    if (FMT == BF) asm("" : "+v"(lane));  // (as above)
+    asm("" : "+v"(lane));  // (as above)
     uint32_t put[NL];  // this wavefront's 16 rows of a tile: where lanes put them
 #pragma unroll
     for (int u = 0; u < NL; ++u) {
