@@ -5,7 +5,7 @@
 // dQ^T += K^T dS^T reads the same K sub-tile transposed.  Delta costs one read of Y here, a launch of its own would cost
 // dY too; the launch of dK and dV that follows reads it.
 //
-// Measured: one document of 16384 tokens, 12 heads of 128, 1092 us, 1130 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 44 us, bound by
+// Measured: one document of 16384 tokens, 12 heads of 128, 1092 us, 1130 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 45 us, bound by
 // what a tile does before and after its blocks of keys.
 #include "packed_tile.h"
 
@@ -146,6 +146,41 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
       half(std::integral_constant<int, SB + T::SUB_B>{}, std::integral_constant<int, SB + 3 * T::SUB_B>{}, k0 + 32, edge);
     }
   };
+  // Y is rounded to bf16, and its error in Delta goes through the sum over k into dQ: of relative size 1 / sqrt(keys of the row), next to the
+  // rounding of dS.  The first rows of a sequence weigh most, so where a row's keys all lie in the first block, Delta is
+  // formed as sum P dP, from that block's products.
+  if (KEPT && steps > 0 && 128 * f.t / p.G + more < 64) {
+    W_VMCNT(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (kg == 0 && wtiles > 0 && first_pos < 64) {
+      float part = 0.f;
+      auto sums = [&](auto ko, auto vo, int k0) {
+        u32x4 fk[KS], fv[KS];
+        p_nat_issue<decltype(ko)::value>(fk, ka);
+        p_nat_issue<decltype(vo)::value>(fv, ka);
+        p_nat_wait(fk);
+        p_nat_wait(fv);
+        f32x16 sa, pa;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) { sa[v] = 0.f; pa[v] = 0.f; }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          sa = mfma(w_frag(fk[ks]), qf[ks], sa);
+          pa = mfma(w_frag(fv[ks]), w_frag(gf[ks]), pa);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) part = fmaf(k0 + key_of(v, hl) > pos ? 0.f : fast_exp2(fmaf(sa[v], c1, nlse2)), pa[v], part);
+      };
+      sums(std::integral_constant<int, 0>{}, std::integral_constant<int, 2 * T::SUB_B>{}, 0);
+      sums(std::integral_constant<int, T::SUB_B>{}, std::integral_constant<int, 3 * T::SUB_B>{}, 32);
+      part = half_sum(part);
+      if (pos < 64) {
+        delta = part;
+        if (live && hl == 0) p.delta_out[di] = delta;
+      }
+    }
+  }
   int i = 0;
   for (; i + 1 < steps; i += 2) {
     step(std::integral_constant<int, 0>{}, i);

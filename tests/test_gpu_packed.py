@@ -212,3 +212,42 @@ def test_two_streams():
     for c in (a, b):
         for n in ("Y", "lse", "dQ", "dK", "dV"):
             assert torch.equal(getattr(c, n), getattr(e, n)), n
+
+
+@pytest.mark.parametrize("D,H,HK", [(64, 8, 2), (128, 6, 2), (128, 40, 8)])
+def test_rows_of_few_keys_have_delta_from_products(D, H, HK):
+    """V = 64 and a little: Y is off by up to a quarter there, and Delta = dY . Y with it by more than dS is large.  Rows of up to 64 keys do
+    not go by it.  Their dS is off by P (the errors of dP and of Delta), which are fp32 sums of D products, and P's own 2^-19; then by half a step
+    of bf16, as the result is."""
+    import torch
+    from packed_cases import Packed
+    print(f"packed delta {D} {H} {HK}", flush=True)
+    lens = [2, 3, 64, 1, 40, 9, 33, 64]
+    c = Packed(29, lens, H, HK, D)
+    rng = np.random.default_rng(30)
+    c.V[:] = torch.from_numpy(64 + 0.5 * rng.integers(0, 9, size=tuple(c.V.shape))).cuda().bfloat16()
+    c.fwd()
+    c.bwd(True)
+    torch.cuda.synchronize()
+    Q, K, V, dY = (c.host(n) for n in ("Q", "K", "V", "dY"))
+    G, half = H // HK, 2.0 ** -8
+    want, bar = {n: np.zeros_like(x) for n, x in (("dQ", Q), ("dK", K))}, {}
+    bar = {n: np.zeros_like(x) for n, x in want.items()}
+    for a, b in zip(c.cu_q[:-1], c.cu_q[1:]):
+        seen = np.tril(np.ones((b - a, b - a), bool))
+        for h in range(H):
+            q, k, v, g = Q[a:b, h], K[a:b, h // G], V[a:b, h // G], dY[a:b, h]
+            s = np.where(seen, q @ k.T * c.scale, -np.inf)
+            P = np.exp(s - s.max(1, keepdims=True))
+            P /= P.sum(1, keepdims=True)
+            dP, e = g @ v.T, D * 2.0 ** -23 * (abs(g) @ abs(v).T)
+            dS = P * (dP - (P * dP).sum(1, keepdims=True))
+            err = P * (e + (P * e).sum(1, keepdims=True) + 2.0 ** -19 * (P * abs(dP)).sum(1, keepdims=True)) + 2.0 ** -19 * abs(dS)
+            err = half * abs(dS) + (1 + half) * err
+            want["dQ"][a:b, h] = c.scale * dS @ k
+            bar["dQ"][a:b, h] = c.scale * err @ abs(k)
+            want["dK"][a:b, h // G] += c.scale * dS.T @ q
+            bar["dK"][a:b, h // G] += c.scale * err.T @ abs(q)
+    for n in ("dQ", "dK"):
+        room = bar[n] * (1 + half) + half * abs(want[n]) + 1e-30
+        assert np.all(abs(c.host(n) - want[n]) <= room), (n, float(np.max(abs(c.host(n) - want[n]) / room)))
