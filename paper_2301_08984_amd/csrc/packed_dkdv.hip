@@ -354,12 +354,18 @@ int row_groups(const PackedP& p) {
 }  // namespace
 
 // Where a launch has few work-groups and sequences are long, the longest of them, which walk most rows, keep the chip waiting: their rows
-// are then cut into two parts.  One part | two | four, us: 6007 tokens x 16 heads of 64 in groups of eight, 11 documents, 214 | 138 | 158.
+// are then cut into two parts, and into four or eight where the work-groups still leave most of the chip idle and a part has some ten steps.
+// One part | two | four | eight, us, the backward: 6007 tokens x 16 heads of 64 in groups of eight, 11 documents (dK and dV alone) 214 | 138 | 158 | -;
+// one sequence of 3000, 8 heads of 128 in one group, 484 | 284 | 182 | 134; 688 tokens, 16 heads in groups of four, 79 | 63 | 56 | 62; 1401 tokens,
+// 16 heads in pairs, 93 | 81 | 96 | 131; 8 of 700 tokens, 12 heads in groups of three (45 MiB of sums), 104 | 125 | 156 | 217.
 int packed_dkdv_parts(const PackedP& p) {
   const int rg = row_groups(p);
   const int64_t groups = ((int64_t)p.Tk * rg >> 7) * p.share_heads, rows = (int64_t)p.Tq * p.G / p.n_seq;
-  if (groups >= 768 || rows < 2048) return 1;
-  return (int64_t)4 * p.Tk * p.share_heads * p.D * 4 > (24 << 20) ? 1 : 2;  // (what the parts' sums may add to the workspace)
+  auto fit = [&](int parts) { return (int64_t)2 * parts * p.Tk * p.share_heads * p.D * 4 <= (24 << 20); };  // (what their sums may add to the workspace)
+  if (groups >= 768 || rows < 2048 || !fit(2)) return 1;
+  int parts = 2;
+  while (parts < 8 && groups * parts < 256 && rows >= 1280 * parts && fit(2 * parts)) parts *= 2;
+  return parts;
 }
 
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st) {

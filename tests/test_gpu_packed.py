@@ -31,6 +31,8 @@ CASES = {
     "parts": ([900, 40], None, 12, 2, 128),
     "parts64": ([1100], [1300], 8, 1, 64),
     "parts_odd_head": ([700, 0, 300], None, 16, 2, 72),
+    "eight_parts": ([1300], None, 8, 1, 128),
+    "eight_parts64": ([1100, 2], [1100, 500], 24, 1, 64),
     "short_rows": ([64] * 95 + [130, 1, 0, 300], None, 32, 16, 128),
     "short_and_long": ([100] * 50 + [400, 0, 700, 33, 129], None, 32, 4, 128),
     "short64": ([107] * 60 + [200, 3], None, 32, 8, 64),
