@@ -32,7 +32,7 @@ int validate(const ss_packed_desc* d) {
   const int64_t G = d->H / d->HK;
   if (G * d->q_stride_h + 33 * d->q_stride_t >= 1000000000ll || G * d->y_stride_h + 33 * d->y_stride_t >= 1000000000ll) return SS_ERR_UNSUPPORTED;
   if (d->Tq > (1 << 30) || d->Tk > (1 << 30) || d->Tq * G >= (1 << 30)) return SS_ERR_UNSUPPORTED;
-  if ((((d->Tq * G > 4ll * d->Tk ? d->Tq * G : 4ll * d->Tk) >> 7) + d->n_seq + 8) * 4 * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
+  if ((((d->Tq * G > 4ll * d->Tk ? d->Tq * G : 4ll * d->Tk) >> 7) + d->n_seq + 8) * 8 * d->HK >= (int64_t)1 << 31) return SS_ERR_UNSUPPORTED;
   if (d->lo < 0 || d->lo >= d->hi || d->hi > d->HK) return SS_ERR_BAD_RANGE;
   if (d->k < 1 || d->k > d->hi - d->lo) return SS_ERR_BAD_K;
   return SS_OK;
