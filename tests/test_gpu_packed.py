@@ -33,6 +33,7 @@ CASES = {
     "parts_odd_head": ([700, 0, 300], None, 16, 2, 72),
     "eight_parts": ([1300], None, 8, 1, 128),
     "eight_parts64": ([1100, 2], [1100, 500], 24, 1, 64),
+    "parts_without_queries": ([2000, 0, 30], [2000, 300, 30], 8, 1, 128),
     "short_rows": ([64] * 95 + [130, 1, 0, 300], None, 32, 16, 128),
     "short_and_long": ([100] * 50 + [400, 0, 700, 33, 129], None, 32, 4, 128),
     "short64": ([107] * 60 + [200, 3], None, 32, 8, 64),
@@ -253,3 +254,30 @@ def test_rows_of_few_keys_have_delta_from_products(D, H, HK):
     for n in ("dQ", "dK"):
         room = bar[n] * (1 + half) + half * abs(want[n]) + 1e-30
         assert np.all(abs(c.host(n) - want[n]) <= room), (n, float(np.max(abs(c.host(n) - want[n]) / room)))
+
+
+def test_parts_captured_and_replayed():
+    """dK and dV in eight parts: a captured call, replayed between eager work, gives the eager call's bits."""
+    import torch
+    from packed_cases import Packed
+    print("packed parts captured", flush=True)
+    a, b = (Packed(31, [1300], 8, 1, 128) for _ in range(2))
+    for c in (a, b):
+        c.fwd()
+        c.bwd(True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.bwd(True)
+    for _ in range(3):
+        for x in (b.dQ, b.dK, b.dV):
+            x.fill_(float("nan"))
+        b.ws.fill_(0xFF)
+        a.bwd(False)
+        graph.replay()
+        torch.cuda.synchronize()
+        a.bwd(True)
+        torch.cuda.synchronize()
+        for n in ("dQ", "dK", "dV"):
+            assert torch.equal(getattr(a, n), getattr(b, n)), n
