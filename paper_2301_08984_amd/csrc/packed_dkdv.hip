@@ -205,7 +205,7 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
       for (int g = 0; g < 4; ++g) pr[g] = u32x4{__float_as_uint(y[4 * g]), __float_as_uint(y[4 * g + 1]), __float_as_uint(y[4 * g + 2]), __float_as_uint(y[4 * g + 3])};
       asm volatile("ds_write_b128 %4, %0 offset:%5\n\tds_write_b128 %4, %1 offset:%6\n\tds_write_b128 %4, %2 offset:%7\n\t"
                    "ds_write_b128 %4, %3 offset:%8"
-                   : : "v"(pr[0]), "v"(pr[1]), "v"(pr[2]), "v"(pr[3]), "v"(pp), "n"(PO), "n"(PO + 1024), "n"(PO + 2048), "n"(PO + 3072)
+                   : : "v"(pr[0]), "v"(pr[1]), "v"(pr[2]), "v"(pr[3]), "v"(pp), "n"(PO), "n"(PO + 1024), "n"(PO + 2048), "n"(PO + 3 * 1024)
                    : "memory");
     }
     of[0] = pack8(&y[0]);
