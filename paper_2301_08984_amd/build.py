@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libss_attn.so")
 SOURCES = ["api.hip", "generic_kernels.hip", "f32_kernels.hip", "mfma_kernels.hip", "small_kernels.hip", "win_fwd.hip", "win_bwd.hip", "fast_fwd.hip", "pair_fwd.hip", "pair_dbias.hip", "fast_fwd128.hip", "fast_stat128.hip", "fast_dq.hip", "fast_rdq.hip", "fast_dq128.hip", "fast_kv128.hip", "fast_wave_fwd.hip", "fast_wave_fwd128.hip", "fast_wave_bwd.hip", "fast_wave_bwd128.hip", "ffn_kernels.hip", "ffn_skinny.hip", "ffn_api.hip", "planner.hip",
-           "fast_dkdv.hip", "packed_api.hip", "packed_fwd.hip", "packed_dq.hip", "packed_dkdv.hip", "cache_api.hip", "cache_rows.hip", "cache_attn.hip", "cache_attn_rows.hip"]
+           "fast_dkdv.hip", "packed_api.hip", "packed_fwd.hip", "packed_delta.hip", "packed_dq.hip", "packed_dkdv.hip", "cache_api.hip", "cache_rows.hip", "cache_attn.hip", "cache_attn_rows.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]
@@ -23,7 +23,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 # that all of a wavefront's registers are vector registers (see the header of fast_wave_fwd128.hip).
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 EXTRA_FLAGS = {"win_fwd.hip": VGPR_FORM, "win_bwd.hip": VGPR_FORM, "pair_dbias.hip": VGPR_FORM, "fast_fwd128.hip": VGPR_FORM, "fast_stat128.hip": VGPR_FORM, "fast_dq128.hip": VGPR_FORM, "fast_kv128.hip": VGPR_FORM, "fast_wave_fwd128.hip": VGPR_FORM, "fast_wave_bwd128.hip": VGPR_FORM,
-               "packed_fwd.hip": VGPR_FORM, "packed_dq.hip": VGPR_FORM, "packed_dkdv.hip": VGPR_FORM, "cache_attn.hip": VGPR_FORM,
+               "packed_fwd.hip": VGPR_FORM, "packed_delta.hip": VGPR_FORM, "packed_dq.hip": VGPR_FORM, "packed_dkdv.hip": VGPR_FORM, "cache_attn.hip": VGPR_FORM,
                "cache_attn_rows.hip": VGPR_FORM}
 
 

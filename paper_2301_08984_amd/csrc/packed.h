@@ -7,7 +7,7 @@
 namespace ssa {
 
 struct PackedP {
-  const void *Q, *K, *V, *Y, *dY;
+  const void *Q, *K, *V, *dY;
   void *Yo, *dQ, *dK, *dV;  // Yo: the forward's output
   const int32_t *cu_q, *cu_k;
   int64_t q_st, q_sh, k_st, k_sh, y_st, y_sh;  // strides of (Q, dQ), (K, V, dK, dV), (Y, dY)
@@ -24,8 +24,8 @@ struct PackedP {
 };
 
 hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st);    // Yo, and lse_out if given
-hipError_t launch_packed_stat(const PackedP& p, hipStream_t st);   // lse_out and delta_out, recomputed
-hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);     // dQ; with Y given delta_out too, else from delta
+hipError_t launch_packed_delta(const PackedP& p, bool kept, hipStream_t st);  // delta_out; from lse where it was kept, else lse_out too
+hipError_t launch_packed_dq(const PackedP& p, hipStream_t st);
 hipError_t launch_packed_dkdv(const PackedP& p, hipStream_t st);
 int packed_dkdv_parts(const PackedP& p);  // from the share, never from the chunk
 

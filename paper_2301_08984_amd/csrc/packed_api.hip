@@ -156,7 +156,7 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
   }
   const Ws w = layout(d, k, kept);
   PackedP p = params(d);
-  p.Q = Q; p.K = K; p.V = V; p.Y = Y; p.dY = dY; p.dQ = dQ; p.dK = dK; p.dV = dV;
+  p.Q = Q; p.K = K; p.V = V; p.dY = dY; p.dQ = dQ; p.dK = dK; p.dV = dV;
   p.cu_q = cu_q; p.cu_k = cu_k ? cu_k : cu_q;
   p.parts = ssa::packed_dkdv_parts(p);
   p.dkdv_parts = (float*)(ws + w.parts);
@@ -166,13 +166,13 @@ int ss_packed_bwd(const ss_packed_desc* d, const void* Q, const void* K, const v
     p.delta_out = (float*)ws;
     p.delta = p.delta_out;
     if (kept) {
-      p.lse = lse;  // (Delta: by the kernel of dQ)
+      p.lse = lse;
     } else {
       p.lse_h0 = p.h0 * p.G;
       p.lse_out = (float*)(ws + w.lse);
       p.lse = p.lse_out;
-      PK_LAUNCH(ssa::launch_packed_stat(p, st), "recompute");
     }
+    PK_LAUNCH(ssa::launch_packed_delta(p, kept, st), "Delta");
     PK_LAUNCH(ssa::launch_packed_dq(p, st), "dQ");
     PK_LAUNCH(ssa::launch_packed_dkdv(p, st), "dK, dV");
   }

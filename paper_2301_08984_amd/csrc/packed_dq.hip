@@ -1,11 +1,10 @@
-// dQ of attention over packed sequences, and Delta = dY . Y of its rows where the forward's output was kept.
+// dQ of attention over packed sequences.
 //
 // The tiles of 128 rows and the buffers of packed_fwd.hip.  Q and dY fragments stay in registers; per block of 32 keys the scores and dP
 // come from the matrix instructions, dS = P (dP - Delta) from the vector ALUs (rounded to bf16, the type of the last product's operands), and
-// dQ^T += K^T dS^T reads the same K sub-tile transposed.  Delta costs one read of Y here, a launch of its own would cost
-// dY too; the launch of dK and dV that follows reads it.
+// dQ^T += K^T dS^T reads the same K sub-tile transposed.
 //
-// Measured: one document of 16384 tokens, 12 heads of 128, 1092 us, 1130 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 45 us, bound by
+// Measured: one document of 16384 tokens, 12 heads of 128, 1052 us, 1175 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 40 us, bound by
 // what a tile does before and after its blocks of keys.
 #include "packed_tile.h"
 
@@ -14,7 +13,7 @@
 namespace ssa {
 namespace {
 
-template <int D, bool KEPT, int KG>
+template <int D, int KG>
 __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   using T = PTile<D>;
   constexpr int KS = T::KS, DB = T::DB, U = T::LOADS / 4, STAGE_B = 4 * T::SUB_B;
@@ -61,33 +60,15 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   const int steps = (ntiles + KG - 1) / KG;  // a group's step i is key tile KG i + kg
   if (steps > 0) fetch_tile(mine, kg);
   const int64_t qrow = (int64_t)(s.q0 + tok) * p.q_st + (int64_t)h * p.q_sh, yrow = (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh;
-  bf16x8 qf[KS];
-  u32x4 gf[KS];
+  bf16x8 qf[KS], gf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     qf[ks] = w_frag(p_signed(p_load8((const uint16_t*)p.Q + qrow, 16 * ks + 8 * hl, p.D), p.scale));
-    gf[ks] = p_load8((const uint16_t*)p.dY + yrow, 16 * ks + 8 * hl, p.D);
+    gf[ks] = w_frag(p_load8((const uint16_t*)p.dY + yrow, 16 * ks + 8 * hl, p.D));
   }
   const float lse = p.lse[(int64_t)(h - p.lse_h0) * p.Tq + s.q0 + tok];
   const float nlse2 = lse == -INFINITY ? lse : -lse * LOG2E;  // no key: every probability is 0
-  float delta;
-  const int64_t di = (int64_t)(h - p.delta_h0) * p.Tq + s.q0 + tok;
-  if (KEPT) {
-    float part = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const u32x4 y = p_load8((const uint16_t*)p.Y + yrow, 16 * ks + 8 * hl, p.D);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        part = fmaf(__uint_as_float(y[e] << 16), __uint_as_float(gf[ks][e] << 16), part);
-        part = fmaf(__uint_as_float(y[e] & 0xffff0000u), __uint_as_float(gf[ks][e] & 0xffff0000u), part);
-      }
-    }
-    delta = half_sum(part);
-    if (live && hl == 0 && kg == 0) p.delta_out[di] = delta;
-  } else {
-    delta = p.delta[di];
-  }
+  const float delta = p.delta[(int64_t)(h - p.delta_h0) * p.Tq + s.q0 + tok];
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -109,7 +90,7 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         sa = mfma(w_frag(fk[ks]), qf[ks], sa);
-        pa = mfma(w_frag(fv[ks]), w_frag(gf[ks]), pa);
+        pa = mfma(w_frag(fv[ks]), gf[ks], pa);
       }
     }
     u32x2 kt_[2][2 * DB];
@@ -146,41 +127,6 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
       half(std::integral_constant<int, SB + T::SUB_B>{}, std::integral_constant<int, SB + 3 * T::SUB_B>{}, k0 + 32, edge);
     }
   };
-  // Y is rounded to bf16, and its error in Delta goes through the sum over k into dQ: of relative size 1 / sqrt(keys of the row), next to the
-  // rounding of dS.  The first rows of a sequence weigh most, so where a row's keys all lie in the first block, Delta is
-  // formed as sum P dP, from that block's products.
-  if (KEPT && steps > 0 && 128 * f.t / p.G + more < 64) {
-    W_VMCNT(0);
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (kg == 0 && wtiles > 0 && first_pos < 64) {
-      float part = 0.f;
-      auto sums = [&](auto ko, auto vo, int k0) {
-        u32x4 fk[KS], fv[KS];
-        p_nat_issue<decltype(ko)::value>(fk, ka);
-        p_nat_issue<decltype(vo)::value>(fv, ka);
-        p_nat_wait(fk);
-        p_nat_wait(fv);
-        f32x16 sa, pa;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) { sa[v] = 0.f; pa[v] = 0.f; }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          sa = mfma(w_frag(fk[ks]), qf[ks], sa);
-          pa = mfma(w_frag(fv[ks]), w_frag(gf[ks]), pa);
-        }
-#pragma unroll
-        for (int v = 0; v < 16; ++v) part = fmaf(k0 + key_of(v, hl) > pos ? 0.f : fast_exp2(fmaf(sa[v], c1, nlse2)), pa[v], part);
-      };
-      sums(std::integral_constant<int, 0>{}, std::integral_constant<int, 2 * T::SUB_B>{}, 0);
-      sums(std::integral_constant<int, T::SUB_B>{}, std::integral_constant<int, 3 * T::SUB_B>{}, 32);
-      part = half_sum(part);
-      if (pos < 64) {
-        delta = part;
-        if (live && hl == 0) p.delta_out[di] = delta;
-      }
-    }
-  }
   int i = 0;
   for (; i + 1 < steps; i += 2) {
     step(std::integral_constant<int, 0>{}, i);
@@ -219,26 +165,23 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
   }
 }
 
-template <int D, bool KEPT, int KG>
+template <int D, int KG>
 __global__ __launch_bounds__(256 * KG, KG == 1 && D == 64 ? 3 : 2) void packed_dq_kernel(PackedP p) {
   __shared__ __attribute__((aligned(1024))) char smem[KG * 2 * 4 * PTile<D>::SUB_B];
-  packed_dq_tile<D, KEPT, KG>(p, smem);
+  packed_dq_tile<D, KG>(p, smem);
 }
 
-template <bool KEPT>
-hipError_t launch(const PackedP& p, hipStream_t st) {
+}  // namespace
+
+hipError_t launch_packed_dq(const PackedP& p, hipStream_t st) {
   const int g = (int)p_blocks(p_most_tiles(p, false, 7), p.h1 - p.h0);
   auto by_groups = [&](auto d) {
-    if (p_two_groups(p)) packed_dq_kernel<d(), KEPT, 2><<<g, 512, 0, st>>>(p);
-    else packed_dq_kernel<d(), KEPT, 1><<<g, 256, 0, st>>>(p);
+    if (p_two_groups(p)) packed_dq_kernel<d(), 2><<<g, 512, 0, st>>>(p);
+    else packed_dq_kernel<d(), 1><<<g, 256, 0, st>>>(p);
   };
   if (p.D <= 64) by_groups(std::integral_constant<int, 64>{});
   else by_groups(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
-
-}  // namespace
-
-hipError_t launch_packed_dq(const PackedP& p, hipStream_t st) { return p.Y ? launch<true>(p, st) : launch<false>(p, st); }
 
 }  // namespace ssa

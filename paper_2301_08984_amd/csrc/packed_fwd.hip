@@ -1,4 +1,4 @@
-// Forward of attention over packed sequences, and the recompute pass of its backward (STAT: LSE and Delta = sum of dY . O instead of Y).
+// Forward of attention over packed sequences.
 //
 // A work-group of four wavefronts owns a tile of 128 rows (packed_tile.h), a wavefront 32 of them, and walks the keys in blocks of 64
 // with the running maximum and sum of a softmax; K / V tiles travel from memory straight into two LDS buffers, one barrier a
@@ -16,7 +16,7 @@
 namespace ssa {
 namespace {
 
-template <int D, bool STAT, int KG>
+template <int D, int KG>
 __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
   using T = PTile<D>;
   constexpr int KS = T::KS, DB = T::DB, U = T::LOADS / 4, STAGE_B = 4 * T::SUB_B;
@@ -191,66 +191,36 @@ __device__ __forceinline__ void packed_fwd_tile(const PackedP& p, char* smem) {
   }
   const float sum = half_sum(l), inv = sum > 0.f ? 1.f / sum : sum;  // no key: 0; NaN stays
   const float lse = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
-  const int64_t stat = (int64_t)(s.q0 + tok);
-  const int64_t yrow = (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh;
-  if (live && hl == 0 && p.lse_out) p.lse_out[(int64_t)(h - p.lse_h0) * p.Tq + stat] = lse;
-  float part = 0.f;
+  if (live && hl == 0 && p.lse_out) p.lse_out[(int64_t)h * p.Tq + s.q0 + tok] = lse;
+  uint16_t* y = (uint16_t*)p.Yo + (int64_t)(s.q0 + tok) * p.y_st + (int64_t)h * p.y_sh;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
-    if (STAT) {
-      const uint16_t* g = (const uint16_t*)p.dY + yrow;
-      uint2 du[4];
+    uint2 o[4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const u32x4 x = p_load8(g, 32 * db + 8 * (2 * j + hl), p.D);
-        auto a = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
-        auto b = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-        du[2 * j] = uint2{a[0], b[0]};
-        du[2 * j + 1] = uint2{a[1], b[1]};
-      }
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4) {
-        const float go[4] = {__uint_as_float(du[g4].x << 16), __uint_as_float(du[g4].x & 0xffff0000u), __uint_as_float(du[g4].y << 16),
-                             __uint_as_float(du[g4].y & 0xffff0000u)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part = fmaf(go[e], oacc[db][4 * g4 + e] * inv, part);
-      }
-    } else {
-      uint2 o[4];
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        o[g4] = pack4_bf16(oacc[db][4 * g4], oacc[db][4 * g4 + 1], oacc[db][4 * g4 + 2], oacc[db][4 * g4 + 3], inv);
-      p_store_row32((uint16_t*)p.Yo + yrow, o, 32 * db, hl, live, p.D);
-    }
-  }
-  if (STAT) {
-    part = half_sum(part);
-    if (live && hl == 0) p.delta_out[(int64_t)(h - p.delta_h0) * p.Tq + stat] = part;
+    for (int g4 = 0; g4 < 4; ++g4)
+      o[g4] = pack4_bf16(oacc[db][4 * g4], oacc[db][4 * g4 + 1], oacc[db][4 * g4 + 2], oacc[db][4 * g4 + 3], inv);
+    p_store_row32(y, o, 32 * db, hl, live, p.D);
   }
 }
 
-template <int D, bool STAT, int KG>
+template <int D, int KG>
 __global__ __launch_bounds__(256 * KG, D == 128 ? 2 : 4) void packed_fwd_kernel(PackedP p) {
   __shared__ __attribute__((aligned(1024))) char smem[KG * 2 * 4 * PTile<D>::SUB_B];
   static_assert(KG == 1 || sizeof(smem) >= 2048 + 4 * 32 * D * 4, "the second group's part fits");
-  packed_fwd_tile<D, STAT, KG>(p, smem);
+  packed_fwd_tile<D, KG>(p, smem);
 }
 
-template <bool STAT>
-hipError_t launch(const PackedP& p, hipStream_t st) {
+}  // namespace
+
+hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st) {
   const int g = (int)p_blocks(p_most_tiles(p, false, 7), p.h1 - p.h0);
   auto by_groups = [&](auto d) {
-    if (p_two_groups(p)) packed_fwd_kernel<d(), STAT, 2><<<g, 512, 0, st>>>(p);
-    else packed_fwd_kernel<d(), STAT, 1><<<g, 256, 0, st>>>(p);
+    if (p_two_groups(p)) packed_fwd_kernel<d(), 2><<<g, 512, 0, st>>>(p);
+    else packed_fwd_kernel<d(), 1><<<g, 256, 0, st>>>(p);
   };
   if (p.D <= 64) by_groups(std::integral_constant<int, 64>{});
   else by_groups(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
-
-}  // namespace
-
-hipError_t launch_packed_fwd(const PackedP& p, hipStream_t st) { return launch<false>(p, st); }
-hipError_t launch_packed_stat(const PackedP& p, hipStream_t st) { return launch<true>(p, st); }
 
 }  // namespace ssa
