@@ -29,6 +29,16 @@ inline int64_t cache_row(int page, int shift, int HK, int h, int64_t pos) {
   return (((int64_t)page * HK + h) << shift) + (pos & ((1 << shift) - 1));
 }
 
+// The keys of units at .. at + take - 1 of a run of `units` units of 1 << sh keys over `len` keys.  (The end of the last unit is not formed
+// from the unit's number: at 2^31 - 1 keys it does not fit.)
+struct CacheSpan { int begin, end; };
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline CacheSpan cache_span(int at, int take, int units, int sh, int len) {
+  return CacheSpan{at << sh, at + take == units ? len : (at + take) << sh};
+}
+
 struct CacheRowsP {  // write, read
   CacheP c;
   void *K, *V;  // bf16, packed tokens

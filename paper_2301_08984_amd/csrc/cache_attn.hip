@@ -127,11 +127,12 @@ __device__ __forceinline__ void cache_attn_run(const CacheAttnP& p, char* smem, 
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[e][v] = 0.f;
   int k0 = begin + 32 * w;
-  if (k0 < end) {
+  bool more = k0 < end;
+  if (more) {
     locate(k0);
     load_v();
   }
-  for (; k0 < end; k0 += 128) {
+  while (more) {  // (positions reach 2^31 - 9: none behind the end is formed)
     live = live_next;
     f32x16 sa;
 #pragma unroll
@@ -154,9 +155,9 @@ __device__ __forceinline__ void cache_attn_run(const CacheAttnP& p, char* smem, 
     float kc[16];  // what makes a score of a product, in base-2 units
 #pragma unroll
     for (int v = 0; v < 16; ++v) kc[v] = FMT == BF ? c1 : c1 * __uint_as_float(ks4[v >> 2][v & 3]);
-    const bool more = k0 + 128 < end;
+    more = end - k0 > 128;
     // all keys are there and none is a new token: nothing to mask
-    const bool plain = live == ~0u && k0 + 32 <= s.before;
+    const bool plain = live == ~0u && s.before - k0 >= 32;
     if (more) locate(k0 + 128);  // K of the next block starts on its way
     bf16x8 pf[2];
     {
@@ -236,7 +237,10 @@ __device__ __forceinline__ void cache_attn_run(const CacheAttnP& p, char* smem, 
         acc[e] = mfma(a.v, pf[t], acc[e]);
       }
     }
-    if (more) load_v();
+    if (more) {
+      load_v();
+      k0 += 128;
+    }
   }
 
   // The wavefronts' parts: maxima and sums first, then O at the common maximum, quarter by quarter of the columns.  acc[e][v] is column
@@ -300,9 +304,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnP p) {
   const Cut cut(p);
   for (int u = piece * cut.each, stop = min(u + cut.each, cut.total); u < stop;) {
     const Run f = cut.find(u);
-    const int take = min(f.units - f.at, stop - u), begin = p.whole ? 0 : 128 * f.at, end = p.whole ? f.s.len : min(begin + 128 * take, f.s.len);
+    const int take = min(f.units - f.at, stop - u);
+    const CacheSpan keys = cache_span(f.at, take, f.units, 7, f.s.len);
     u += take;
-    cache_attn_run<FMT, D>(p, smem, f, hk, begin, end, take == f.units, part_slot(piece, cut.each, f.first));
+    cache_attn_run<FMT, D>(p, smem, f, hk, keys.begin, keys.end, take == f.units, part_slot(piece, cut.each, f.first));
   }
 }
 

@@ -35,7 +35,7 @@ __device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rb = w % RB, kg = w / RB;
   const CacheSeq s = f.s;
   const int rows = s.n * p.G, row0 = 128 * f.group, shift = p.c.shift;
-  const int steps = (end - begin + 63) >> 6;  // of 64 keys
+  const int steps = end > begin ? ((end - begin - 1) >> 6) + 1 : 0;  // of 64 keys
 
   const int32_t* line = p.c.table + (int64_t)f.b * p.c.max_pages;
   const int last_entry = (end - 1) >> shift;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void cache_rows_run(const CacheAttnP& p, char* smem, 
     scores(std::integral_constant<int, 0>{});
     if constexpr (NKB == 2) scores(std::integral_constant<int, NKB - 1>{});
     const float* sc = (const float*)(smem + L::SCALES + (2 * kg + decltype(buffer)::value) * 512) + 4 * hl;
-    const bool plain = there == (NKB == 2 ? ~0ull : 0xffffffffull) && k0 + KEYS <= s.before;
+    const bool plain = there == (NKB == 2 ? ~0ull : 0xffffffffull) && s.before - k0 >= KEYS;
     uint32_t seen[NKB];
     float rmax = -INFINITY;
 #pragma unroll
@@ -319,11 +319,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnP p) {
   for (int u = piece * cut.each, stop = min(u + cut.each, cut.total); u < stop;) {
     const Run f = cut.find(u);
     const int sh = Cut::many(p, f.s.n) ? 6 : 7, take = min(f.units - f.at, stop - u);
-    const int begin = p.whole ? 0 : f.at << sh, end = p.whole ? f.s.len : min(begin + (take << sh), f.s.len);
+    const CacheSpan keys = cache_span(f.at, take, f.units, sh, f.s.len);
     u += take;
     const int slot = part_slot(piece, cut.each, f.first);
-    if (sh == 6) cache_rows_run<FMT, D, 4>(p, smem, f, hk, begin, end, take == f.units, slot);
-    else cache_rows_run<FMT, D, 2>(p, smem, f, hk, begin, end, take == f.units, slot);
+    if (sh == 6) cache_rows_run<FMT, D, 4>(p, smem, f, hk, keys.begin, keys.end, take == f.units, slot);
+    else cache_rows_run<FMT, D, 2>(p, smem, f, hk, keys.begin, keys.end, take == f.units, slot);
   }
 }
 
