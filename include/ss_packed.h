@@ -76,6 +76,9 @@ int ss_packed_fwd(const ss_packed_desc* desc, const void* Q, const void* K, cons
  *   Y, lse in : as the forward wrote them, or both NULL: recomputed chunk by chunk (one without the other:
  *               SS_ERR_NULL).  What is used is lse: Delta is formed from the products that dS is formed from, sum_j P_ij <dY_i, v_j>,
  *               not from the rounded Y, whose error would show in dQ wherever the keys have a mean or one key has most of a row.
+ *   Q, dY  in : in rows of other sequences, of no sequence, and of queries that see no key they may be anything.  Inside a
+ *               sequence those of a query that sees a key have to be finite (for the keys that it does not see they are multiplied by
+ *               a probability of zero).
  *   dQ, dK, dV out: the rows of the sequences, heads of the share; other rows are left as they were.
  *   workspace : at least bwd_bytes, 256-byte aligned; need not start at zero. */
 int ss_packed_bwd(const ss_packed_desc* desc, const void* Q, const void* K, const void* V, const int32_t* cu_q,

@@ -109,7 +109,7 @@ __device__ __forceinline__ void packed_kv_wave(const PackedP& p, char* smem, con
     for (int u = 0; u < NR; ++u) {
       const int rho = T::ROWS * ((mate + MATES * u) % T::LOADS) + lane / T::CHUNKS;
       const uint32_t dt = (uint32_t)(mine[u].tok - base.tok), g = (uint32_t)mine[u].g;
-      const bool there = rho < left && c16[u] != P_NOWHERE;
+      const bool there = rho < left && mine[u].tok + more >= 0 && c16[u] != P_NOWHERE;  // (a row that sees no key may hold anything)
       oq[u] = there ? dt * qs2 + g * qh2 + c16[u] : P_NOWHERE;
       oy[u] = there ? dt * ys2 + g * yh2 + c16[u] : P_NOWHERE;
       mine[u].step(G, dtok, dg);

@@ -64,7 +64,7 @@ __device__ __forceinline__ void packed_dq_tile(const PackedP& p, char* smem) {
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     qf[ks] = w_frag(p_signed(p_load8((const uint16_t*)p.Q + qrow, 16 * ks + 8 * hl, p.D), p.scale));
-    gf[ks] = w_frag(p_load8((const uint16_t*)p.dY + yrow, 16 * ks + 8 * hl, p.D));
+    gf[ks] = w_frag(p_load8((const uint16_t*)p.dY + yrow, 16 * ks + 8 * hl, pos >= 0 ? p.D : 0));  // (a row that sees no key may hold anything)
   }
   const float lse = p.lse[(int64_t)(h - p.lse_h0) * p.Tq + s.q0 + tok];
   const float nlse2 = lse == -INFINITY ? lse : -lse * LOG2E;  // no key: every probability is 0
