@@ -58,7 +58,7 @@ int ss_cache_write(const ss_cache_desc* desc, int32_t T, const void* K, const vo
                    void* v_codes, float* v_scales, void* hip_stream);
 
 /* Reads rows back as bf16 (rounded once), packed as ss_packed_fwd takes its keys: row cu[b] + i of K and V is position
- * start[b] + i (start NULL: 0) of sequence b.  Rows outside cu[0] .. cu[n_seq]-1 are left as they were. */
+ * start[b] + i (start NULL: 0) of sequence b (cu clamped to 0 .. T).  Rows outside cu[0] .. cu[n_seq]-1 are left as they were. */
 int ss_cache_read(const ss_cache_desc* desc, int32_t T, const int32_t* cu, const int32_t* start, const int32_t* table,
                   const void* k_codes, const float* k_scales, const void* v_codes, const float* v_scales, void* K, void* V,
                   int64_t stride_t, int64_t stride_h, void* hip_stream);

@@ -28,7 +28,7 @@ __device__ __forceinline__ int place_of(const CacheRowsP& p, int t, Place& at) {
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) {
     const int i = min(b0 + lane, p.c.n_seq - 1);
-    const int from = p.cu[i], to = p.cu[i + 1], start = p.start ? p.start[i] : 0;
+    const int from = max(p.cu[i], 0), to = p.cu[i + 1], start = p.start ? p.start[i] : 0;
     const uint64_t hit = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.n_seq && from <= t && t < to);
     if (!hit) continue;
     const int l = 63 - __builtin_clzll(hit);
