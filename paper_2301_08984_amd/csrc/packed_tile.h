@@ -228,11 +228,18 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
 // (row tiles: 128 * tiles <= Tq * G + 127 * n_seq; key tiles alike)
 inline int64_t p_most_tiles(const PackedP& p, bool keys, int sh) { return ((keys ? (int64_t)p.Tk : (int64_t)p.Tq * p.G) >> sh) + p.n_seq; }
 
-// Two groups of wavefronts share a tile of rows where there are too few tiles to keep the chip busy to the end with one: the longest tile then
-// takes half as long.  One group | two, us, tiles x heads: 6 turns of 2000 tokens over a cache, 32 heads, 165 | 131; 11 documents, 16 heads of 64
-// in groups of eight, backward, 318 | 306; but 23 documents of 8192 tokens, 12 heads in groups of three, 131 | 167, and 19 prompts
-// of 9001 tokens, 32 heads, 91 | 124 (two groups cost a join and half of the work-groups on a CU).
-inline bool p_two_groups(const PackedP& p) { return (((int64_t)p.Tq * p.G) >> 7) * p.share_heads < 640; }
+// Two groups of wavefronts share a tile of rows where the longest tile is what a launch lasts: it then takes half as long.  They cost a join at the end,
+// and one work-group fits a compute unit where two of one group do, so there have to be at most as many tiles as the chip holds of one group (512; heads of 64:
+// more, but their backward has the registers of 256 to 768), and tiles have to be long, which is known of the mean sequence only.  One group | two, us, the forward (the
+// backward and heads of 64 turn at the same places), 32 heads in groups of four unless said otherwise, tiles x heads first:
+//   64: 2 sequences of 128 tokens 8.4 | 9.4, 1 of 512 (16 heads on 2) 15.2 | 14.2; 200: 5 of 160 10.1 | 11.4, 2 of 400 13.5 | 13.3, 1 of 1600 (16 on 2) 33.7 | 28.1
+//   256: 3 of 341 13.6 | 17.2, 1 of 1024 24.6 | 21.9; 320: 2 of 640 19.7 | 20.1, 1 of 1280 30.2 | 25.3; 400: 2 of 800 23.8 | 25.0, 1 of 1600 37.4 | 33.5
+//   512: 3 of 682 23.6 | 33.7, 1 of 2048 49.5 | 45.7; 600: 2 of 2400 (16 on 2) 59.8 | 65.8; 768: 1 of 3072 86.3 | 94.1
+// (11 documents, 16 heads of 64 in groups of eight, 750 tiles, one group by this rule: forward 38.0 | 31.2, backward 168.2 | 166.4.)
+inline bool p_two_groups(const PackedP& p) {
+  const int64_t tiles = (((int64_t)p.Tq * p.G) >> 7) * p.share_heads, keys = p.Tk / p.n_seq;
+  return tiles < 256 ? keys >= 400 : tiles <= 512 && keys >= 3 * tiles;
+}
 
 // 1 / ln 2 times the scale, never zero: a factor of 0 would make NaN of a masked score; any score times 2^-120 is 0
 // next to the exponents that matter.  Its sign goes into Q.
