@@ -404,7 +404,14 @@ void launch_join(const CacheAttnP& p, hipStream_t st) {
   else cache_join_kernel<D, 1><<<(int)((units + 3) / 4), 256, 0, st>>>(p);
 }
 
-// How the work is cut (cache_cut.h): from the descriptors alone.
+// How the work is cut (cache_cut.h): from the descriptors alone, so from the table's room, not from the lengths.
+// Up to 512 keys of room one launch finishes every sequence; beyond that four wavefronts over a whole sequence take longer than pieces and the launch that joins
+// them.  One launch | pieces and join, us, bf16, sequences as long as the table has room, heads of 128:
+//   1 sequence, 4 key heads, 4 rows: 256 keys 7.7 | 9.5, 512 10.4 | 10.9, 1024 15.6 | 10.9, 4096 46 | 11; 64 rows: 256 10.3 | 12.1, 512 15.3 | 14.1, 1024 24.9 | 14.1
+//   8 sequences, 8 key heads, 4 rows: 256 8.1 | 9.9, 512 10.7 | 11.2, 1024 16.7 | 12.5; 64 rows: 256 10.6 | 13.3, 512 15.8 | 15.7, 1024 26.3 | 18.7
+//   64 sequences, 8 key heads, 4 rows: 256 15.0 | 17.8, 512 24.3 | 26.9, 1024 43.6 | 45.5 (equal lengths, as many runs as the chip holds)
+// A piece has two units at least: one unit | two | four, us, 8 sequences of 8 key heads, 4 rows, room for 4096: 60 keys 8.3 | 12.1 | 19.8, 200 keys 9.7 | 9.9 | 15.2, 500 keys
+// 10.2 | 11.4 | 12.7; but 32 sequences, 64 rows: 200 keys 25.6 | 19.3 | 27.7, and 4 sequences of 384 rows and 120 keys 22.7 | 14.8 | 21.6, where one unit has parts to join.
 void cut(CacheAttnP& p) {
   p.max_rows = p.max_new * p.G;
   p.whole = ((int64_t)p.c.max_pages << p.c.shift) <= 512;
