@@ -42,6 +42,16 @@ struct Run {  // over the keys of one sequence, for its rows of group `group`
   CacheSeq s;
   int b, group, first, units, at;  // `first`: its first unit on the line; `units` it has; `at`: the unit asked for, from there
 };
+__host__ __device__ __forceinline__ bool cut_many(int n, int G) { return n * G > 64; }
+// units of one run of a sequence with n new tokens and len keys, and its runs
+__host__ __device__ __forceinline__ int cut_units(bool whole, int n, int G, int len) {
+  return whole || len <= 0 ? 1 : ((len - 1) >> (cut_many(n, G) ? 6 : 7)) + 1;
+}
+__host__ __device__ __forceinline__ int cut_runs(int n, int G) { return n <= 0 ? 0 : cut_many(n, G) ? (n * G + 127) >> 7 : 1; }
+__host__ __device__ __forceinline__ int cut_each(int least, int total, int pieces) {
+  const int even = (total + pieces - 1) / pieces;
+  return even > least ? even : least;
+}
 struct Cut {
   const CacheAttnP& p;
   CacheSeq mine;     // of the first 64 sequences, a lane each
@@ -50,15 +60,11 @@ struct Cut {
     const int lane = threadIdx.x & 63;
     mine = at_lane(lane);
     for (int b0 = 0; b0 < p.c.n_seq; b0 += 64) total += __builtin_amdgcn_readlane(scan64(line(b0 ? at_lane(b0 + lane) : mine)), 63);
-    each = max(p.least, (total + p.pieces - 1) / p.pieces);
+    each = cut_each(p.least, total, p.pieces);
   }
-  __device__ __forceinline__ static bool many(const CacheAttnP& p, int n) { return n * p.G > 64; }
-  __device__ __forceinline__ int units(const CacheSeq& s) const {  // of one run
-    if (p.whole) return 1;
-    const int sh = many(p, s.n) ? 6 : 7;
-    return s.len > 0 ? ((s.len - 1) >> sh) + 1 : 1;
-  }
-  __device__ __forceinline__ int line(const CacheSeq& s) const { return s.n > 0 ? units(s) * (many(p, s.n) ? (s.n * p.G + 127) >> 7 : 1) : 0; }
+  __device__ __forceinline__ static bool many(const CacheAttnP& p, int n) { return cut_many(n, p.G); }
+  __device__ __forceinline__ int units(const CacheSeq& s) const { return cut_units(p.whole, s.n, p.G, s.len); }  // of one run
+  __device__ __forceinline__ int line(const CacheSeq& s) const { return units(s) * cut_runs(s.n, p.G); }
   __device__ __forceinline__ CacheSeq at_lane(int b) const {
     CacheSeq s = cache_seq(p, min(b, p.c.n_seq - 1));
     if (b >= p.c.n_seq) s.n = s.len = 0;
@@ -119,7 +125,7 @@ struct Cut {
   }
 };
 // A piece's first run may have begun in an earlier piece, its last one may go on in the next: two slots for parts a piece.
-__device__ __forceinline__ int part_slot(int piece, int each, int first) { return 2 * piece + (first > piece * each ? 1 : 0); }
+__host__ __device__ __forceinline__ int part_slot(int piece, int each, int first) { return 2 * piece + (first > piece * each ? 1 : 0); }
 // where a part's row lies in the workspace, in rows
 __host__ __device__ __forceinline__ int64_t part_row(const CacheAttnP& p, int slot, int hk, int row) {
   return ((int64_t)slot * p.c.HK + hk) * p.part_rows + row;

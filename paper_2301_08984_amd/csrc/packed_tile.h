@@ -128,8 +128,8 @@ __device__ __forceinline__ int p_total(int x) { return __builtin_amdgcn_readlane
 // stay in its L2; of the heads left over 4, 2 and 1 at a time are spread over 2, 4 or 8 XCDs by the rank of their tiles.  Tiles go
 // by rank (the heaviest first), the heads of one rank next to each other.
 struct PPlace { int rank, head; };
-__device__ __forceinline__ PPlace p_place(int HK) {
-  const int x = blockIdx.x & 7, idx = blockIdx.x >> 3, q = idx / HK, a = HK >> 3;
+__host__ __device__ __forceinline__ PPlace p_place_of(int block, int HK) {
+  const int x = block & 7, idx = block >> 3, q = idx / HK, a = HK >> 3;
   int rem = idx - q * HK;
   PPlace o;
   if (rem < 8 * a) {
@@ -151,6 +151,7 @@ __device__ __forceinline__ PPlace p_place(int HK) {
   }
   return PPlace{8 * q + x, first};
 }
+__device__ __forceinline__ PPlace p_place(int HK) { return p_place_of((int)blockIdx.x, HK); }
 inline int64_t p_blocks(int64_t tiles, int HK) { return (tiles + 7) / 8 * 8 * HK; }
 
 // The tile of rank `rank`: its sequence, and its number in it (-1: fewer tiles than that).  KEYS: tiles of 1 << SH keys, else of 1 << SH
@@ -160,13 +161,13 @@ inline int64_t p_blocks(int64_t tiles, int HK) { return (tiles + 7) / 8 * 8 * HK
 // bisection.  With more sequences tiles are in the order of the sequences.
 struct PFound { PackedSeq s; int t; };
 template <bool KEYS, int SH>
-__device__ __forceinline__ int p_tiles(const PackedSeq& s, int G) { return ((KEYS ? s.m : s.n * G) + (1 << SH) - 1) >> SH; }
+__host__ __device__ __forceinline__ int p_tiles(const PackedSeq& s, int G) { return ((KEYS ? s.m : s.n * G) + (1 << SH) - 1) >> SH; }
 template <bool KEYS, int SH>
-__device__ __forceinline__ int p_steps(const PackedSeq& s, int G) {  // of the sequence's heaviest tile
+__host__ __device__ __forceinline__ int p_steps(const PackedSeq& s, int G) {  // of the sequence's heaviest tile
   return KEYS ? (s.n * G + 31) >> 5 : (s.m + 63) >> 6;
 }
 template <bool KEYS, int SH>
-__device__ __forceinline__ int p_at_least(const PackedSeq& s, int G, int L) {  // tiles with L steps or more
+__host__ __device__ __forceinline__ int p_at_least(const PackedSeq& s, int G, int L) {  // tiles with L steps or more
   const int tiles = p_tiles<KEYS, SH>(s, G), more = s.m - s.n;
   if (L <= 0) return tiles;
   if (KEYS) {
@@ -176,6 +177,22 @@ __device__ __forceinline__ int p_at_least(const PackedSeq& s, int G, int L) {  /
   const int y = 64 * (L - 1) - more;  // the first token that sees as many keys
   return y >= s.n ? 0 : tiles - ((max(y, 0) * G) >> SH);
 }
+// The steps of the tile of rank `rank` when they are in order of their steps, at most `most` (count(L): tiles with L steps or more): more than `rank` tiles
+// have that many or more, not as many have more.
+template <typename Count>
+__host__ __device__ __forceinline__ int p_level(int rank, int most, Count&& count) {
+  int lo = 0, hi = most + 1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (count(mid) > rank) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+// The number in its sequence of `tiles` tiles of the i-th tile with exactly some number of steps, when `above` have more: a sequence's first tiles of
+// keys, and its last tiles of rows, have most steps.
+template <bool KEYS>
+__host__ __device__ __forceinline__ int p_number(int tiles, int above, int i) { return KEYS ? above + i : tiles - 1 - above - i; }
 template <bool KEYS, int SH>
 __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
   const int lane = threadIdx.x & 63, G = p.G;
@@ -195,19 +212,13 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
   if (p.n_seq <= 64) {
     const PackedSeq s = of_lane(0);
     if (rank >= p_total(p_tiles<KEYS, SH>(s, G))) return f;
-    int lo = 0, hi = p_steps<KEYS, SH>(s, G);
-    hi = p_max(hi) + 1;
-    while (hi - lo > 1) {  // more than `rank` tiles have `lo` steps or more, not as many have `hi`
-      const int mid = (lo + hi) >> 1;
-      if (p_total(p_at_least<KEYS, SH>(s, G, mid)) > rank) lo = mid;
-      else hi = mid;
-    }
-    const int above = p_at_least<KEYS, SH>(s, G, hi), mine = p_at_least<KEYS, SH>(s, G, lo) - above;
+    const int level = p_level(rank, p_max(p_steps<KEYS, SH>(s, G)), [&](int L) { return p_total(p_at_least<KEYS, SH>(s, G, L)); });
+    const int above = p_at_least<KEYS, SH>(s, G, level + 1), mine = p_at_least<KEYS, SH>(s, G, level) - above;
     const int left = rank - p_total(above), upto = p_scan(mine);
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > left));
     from(s, l);
     const int i = left - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)), ab = __builtin_amdgcn_readlane(above, l);
-    f.t = KEYS ? ab + i : p_tiles<KEYS, SH>(f.s, G) - 1 - ab - i;
+    f.t = p_number<KEYS>(p_tiles<KEYS, SH>(f.s, G), ab, i);
     return f;
   }
   for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
@@ -220,7 +231,7 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > rank));
     from(s, l);
     const int i = rank - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
-    f.t = KEYS ? i : p_tiles<KEYS, SH>(f.s, G) - 1 - i;
+    f.t = p_number<KEYS>(p_tiles<KEYS, SH>(f.s, G), 0, i);
     return f;
   }
   return f;

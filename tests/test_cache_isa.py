@@ -1,5 +1,5 @@
 """The kernels over the cache that keep keys and values in registers: nothing is spilled to memory and no accumulation register is in use, in any
-format and head size (e4m3 at 128 takes 255 of 256 registers)."""
+format and head size (e4m3 at 128 takes nearly all of 256 registers)."""
 import os
 import subprocess
 
