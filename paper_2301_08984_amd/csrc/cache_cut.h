@@ -2,6 +2,7 @@
 #pragma once
 #include "cache.h"
 #include "mfma_common.h"
+#include "wave_scan.h"
 
 namespace ssa {
 namespace {
@@ -20,15 +21,6 @@ __device__ __forceinline__ CacheSeq cache_seq(const CacheAttnP& p, int b) {
   s.before = max(lens - n, 0);
   s.len = (int)min((int64_t)lens, (int64_t)p.c.max_pages << p.c.shift);  // keys that the table has a place for
   return s;
-}
-__device__ __forceinline__ int scan64(int x) {  // inclusive prefix sums over the wavefront
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
 }
 
 // How the work is cut.  All keys of all sequences, for one key head, are one line of units, a unit being 128 keys (64 where a sequence has

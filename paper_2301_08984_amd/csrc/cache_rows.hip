@@ -4,7 +4,6 @@
 // its K rows, one a head, and V rows behind them).  The largest magnitude goes round the row's lanes, every lane converts its
 // own eight values.  Bound by memory: 4 D bytes in and 2 D + 8 out for a token and head, or the reverse.
 #include "cache.h"
-#include "packed.h"
 #include "mfma_common.h"
 
 namespace ssa {
@@ -17,7 +16,7 @@ __device__ inline float fp8_scale(float most) {
   return exp2_int(max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -126));
 }
 
-// What a wavefront does: rows `first` .. of token t, and where they lie in the cache.
+// Where a token lies in the cache.
 struct Place {
   int page;  // -1: none
   int64_t pos;

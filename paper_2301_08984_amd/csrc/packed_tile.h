@@ -13,6 +13,7 @@
 #pragma once
 #include "packed.h"
 #include "wave_dma.h"
+#include "wave_scan.h"
 
 namespace ssa {
 namespace {
@@ -103,16 +104,6 @@ __device__ __forceinline__ u32x4 p_load8(const uint16_t* row_ptr, int col, int D
   return col < D ? *(const u32x4*)(row_ptr + col) : u32x4{0, 0, 0, 0};
 }
 
-// inclusive prefix sums over the wavefront
-__device__ __forceinline__ int p_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1 .. 8: within 16 lanes
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15, :31: the rows before
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
 __device__ __forceinline__ int p_max(int x) {  // of the wavefront's non-negative numbers
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
@@ -122,7 +113,7 @@ __device__ __forceinline__ int p_max(int x) {  // of the wavefront's non-negativ
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
   return __builtin_amdgcn_readlane(x, 63);
 }
-__device__ __forceinline__ int p_total(int x) { return __builtin_amdgcn_readlane(p_scan(x), 63); }
+__device__ __forceinline__ int p_total(int x) { return __builtin_amdgcn_readlane(scan64(x), 63); }
 
 // A launch's work-groups: 8 XCDs with an L2 each are dealt them in turn.  Every XCD gets HK / 8 whole key heads, whose K and V
 // stay in its L2; of the heads left over 4, 2 and 1 at a time are spread over 2, 4 or 8 XCDs by the rank of their tiles.  Tiles go
@@ -214,7 +205,7 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
     if (rank >= p_total(p_tiles<KEYS, SH>(s, G))) return f;
     const int level = p_level(rank, p_max(p_steps<KEYS, SH>(s, G)), [&](int L) { return p_total(p_at_least<KEYS, SH>(s, G, L)); });
     const int above = p_at_least<KEYS, SH>(s, G, level + 1), mine = p_at_least<KEYS, SH>(s, G, level) - above;
-    const int left = rank - p_total(above), upto = p_scan(mine);
+    const int left = rank - p_total(above), upto = scan64(mine);
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > left));
     from(s, l);
     const int i = left - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)), ab = __builtin_amdgcn_readlane(above, l);
@@ -223,7 +214,7 @@ __device__ __forceinline__ PFound p_find(const PackedP& p, int rank) {
   }
   for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
     const PackedSeq s = of_lane(b0);
-    const int mine = p_tiles<KEYS, SH>(s, G), upto = p_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+    const int mine = p_tiles<KEYS, SH>(s, G), upto = scan64(mine), all = __builtin_amdgcn_readlane(upto, 63);
     if (rank >= all) {
       rank -= all;
       continue;
