@@ -6,7 +6,8 @@
  *
  *   SS_CACHE_FP8  codes in e4m3 (finite, largest 448); scale = the smallest power of two s >= 2^-126 with
  *                 max |x| <= 448 s.  A power of two, so that neither x / s nor the product that is read back is
- *                 rounded: what the format loses is the code's own rounding (at most 2^-4 of a value).
+ *                 rounded: what the format loses is the code's own rounding, at most max(2^-4 |x|, 2^-10 scale) (below
+ *                 2^-6 scale codes are subnormal: steps of 2^-9 scale).
  *   SS_CACHE_INT8 codes -127 .. 127; scale = max(max |x| / 127, 2^-126).
  *   code = round to nearest even of x / scale (the quotient in fp32); value = code * scale.
  *   A row of zeros has scale 1.  A row that holds a NaN or an infinity gets a scale of NaN, so that it shows.

@@ -36,7 +36,8 @@ extern "C" {
 /* Element (t, h, d) of Q and dQ is at t*q_stride_t + h*q_stride_h + d, of K, V, dK and dV at
  * t*k_stride_t + h*k_stride_h + d, of Y and dY at t*y_stride_t + h*y_stride_h + d (in elements, d contiguous), so
  * that Q, K and V may be slices of one buffer.  Strides are multiples of 8 elements, at least D and below 2^24;
- * base pointers 16-byte aligned; D a multiple of 8 up to 128 (64 and 128 waste nothing). */
+ * base pointers 16-byte aligned; D a multiple of 8 up to 128 (64 and 128 waste nothing).  A step's rows lie within a lane's reach:
+ * H/HK * stride_h + 33 * stride_t < 10^9, of Q and of Y; rows are counted in 30 bits: Tk at most and Tq * H/HK below 2^30. */
 typedef struct {
   int32_t Tq, Tk;    /* tokens (rows) of Q, Y, dY, dQ, and of K, V, dK, dV           */
   int32_t n_seq;     /* sequences, up to 65535                                       */

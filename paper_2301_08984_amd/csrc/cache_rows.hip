@@ -157,7 +157,7 @@ hipError_t with_format(const CacheP& c, F&& f) {
 }
 
 // Wavefronts of a token, and work-groups of the launch: one wavefront for four (eight) rows while those are few, one for a token's rows
-// where there are tokens enough.  One | several: 31200 tokens of 8 heads read back 32.0 | 36.9 us (6.3 TB/s with reads and writes together), one step's 64
+// where there are tokens enough.  One | several: 31200 tokens of 8 heads read back 32.0 | 36.9 us (6.05 TB/s with reads and writes together), one step's 64
 // tokens written 7.9 | 5.1.
 int cut(CacheRowsP& p) {
   const int rows = 512 / p.c.D;

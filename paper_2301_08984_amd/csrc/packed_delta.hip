@@ -9,8 +9,8 @@
 // The tiles of 128 rows and the buffers of packed_fwd.hip, and its running maximum where LSE is not known; no product needs K or V
 // transposed, and a row keeps three numbers in place of its output.
 //
-// Measured: one document of 16384 tokens, 12 heads of 128, 746 us, 1100 TFLOP/s (a large library product: 1216), bound by the matrix instructions of two
-// products; 23 documents, 8192 tokens, 12 heads in groups of three, 31 us; 11 documents, 6007 tokens, 16 heads of 64 in groups of eight, with LSE, 58 us.
+// Measured: one document of 16384 tokens, 12 heads of 128, 759 us, 1085 TFLOP/s (a large library product: 1216), bound by the matrix instructions of two
+// products; 23 documents, 8192 tokens, 12 heads in groups of three, 30 us; 11 documents, 6007 tokens, 16 heads of 64 in groups of eight, with LSE, 57 us.
 #include "packed_tile.h"
 
 #include <type_traits>

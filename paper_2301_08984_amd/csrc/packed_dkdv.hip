@@ -361,7 +361,7 @@ int row_groups(const PackedP& p) {
 int packed_dkdv_parts(const PackedP& p) {
   const int rg = row_groups(p);
   const int64_t groups = ((int64_t)p.Tk * rg >> 7) * p.share_heads, rows = (int64_t)p.Tq * p.G / p.n_seq;
-  auto fit = [&](int parts) { return (int64_t)2 * parts * p.Tk * p.share_heads * p.D * 4 <= (24 << 20); };  // (what their sums may add to the workspace)
+  auto fit = [&](int parts) { return (int64_t)2 * parts * p.Tk * p.share_heads * p.D * 4 <= (24 << 20); };  // (what their sums may add to the workspace; it keeps out, too, where the sums cost more than the parts give, as the last example above)
   if (groups >= 768 || rows < 2048 || !fit(2)) return 1;
   int parts = 2;
   while (parts < 8 && groups * parts < 256 && rows >= 1280 * parts && fit(2 * parts)) parts *= 2;

@@ -4,7 +4,7 @@
 // come from the matrix instructions, dS = P (dP - Delta) from the vector ALUs (rounded to bf16, the type of the last product's operands), and
 // dQ^T += K^T dS^T reads the same K sub-tile transposed.
 //
-// Measured: one document of 16384 tokens, 12 heads of 128, 1052 us, 1175 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 40 us, bound by
+// Measured: one document of 16384 tokens, 12 heads of 128, 1071 us, 1155 TFLOP/s; 23 documents, 8192 tokens, 12 heads in groups of three: 40 us, bound by
 // what a tile does before and after its blocks of keys.
 #include "packed_tile.h"
 
