@@ -236,7 +236,7 @@ inline int64_t p_most_tiles(const PackedP& p, bool keys, int sh) { return ((keys
 // backward and heads of 64 turn at the same places), 32 heads in groups of four unless said otherwise, tiles x heads first:
 //   64: 2 sequences of 128 tokens 8.4 | 9.4, 1 of 512 (16 heads on 2) 15.2 | 14.2; 200: 5 of 160 10.1 | 11.4, 2 of 400 13.5 | 13.3, 1 of 1600 (16 on 2) 33.7 | 28.1
 //   256: 3 of 341 13.6 | 17.2, 1 of 1024 24.6 | 21.9; 320: 2 of 640 19.7 | 20.1, 1 of 1280 30.2 | 25.3; 400: 2 of 800 23.8 | 25.0, 1 of 1600 37.4 | 33.5
-//   512: 3 of 682 23.6 | 33.7, 1 of 2048 49.5 | 45.7; 600: 2 of 2400 (16 on 2) 59.8 | 65.8; 768: 1 of 3072 86.3 | 94.1
+//   512: 3 of 682 23.6 | 33.7, 1 of 2048 49.5 | 45.7; 600: 2 of 2400 (16 on 2) 59.8 | 65.8; 768: 2 of 1536 51.5 | 58.8
 // (11 documents of up to 3300 tokens, 16 heads of 64 in groups of eight, 750 tiles, one group by this rule: Delta 57.7 | 58.2, dQ 67.5 | 66.5; of up to 2300: forward 38.0 | 31.2.)
 inline bool p_two_groups(const PackedP& p) {
   const int64_t tiles = (((int64_t)p.Tq * p.G) >> 7) * p.share_heads, keys = p.Tk / p.n_seq;
